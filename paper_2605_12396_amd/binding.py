@@ -34,6 +34,16 @@ class ReaOpts(C.Structure):
                 ("huff_ps_per_byte", C.c_uint32), ("reserved", C.c_uint32)]
 
 
+F32, BF16, F16 = range(3)                               # nz_float_type
+MX4_NEAREST, MX4_STOCHASTIC = range(2)                  # nz_mx4_rounding
+MX4_PRODUCT, MX4_LINEAR, MX4_GRAD = range(3)            # nz_mx4_kind
+_FLOAT_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class Mx4Matrix(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("pitch", C.c_size_t)]
+
+
 RESULT_BYTES = 32   # sizeof(nz_result)
 REA_RESULT_BYTES = 40   # sizeof(nz_rea_result)
 _lib = None
@@ -90,6 +100,25 @@ def lib():
         L.nz_reduce_local_sr.argtypes = [vp, sz, vp, vp, sz, sz, f32, C.c_uint32, vp, po, vp, sz, vp]
         L.nz_reduce_local_sr.restype = C.c_int
         L.nz_reduce_local.restype = C.c_int
+        pm = C.POINTER(Mx4Matrix)
+        L.nz_mx4_pitch.argtypes = [sz]
+        L.nz_mx4_pitch.restype = sz
+        L.nz_mx4_quantize.argtypes = [vp, C.c_int, sz, sz, sz, C.c_int, C.c_uint32, pm, vp]
+        L.nz_mx4_quantize.restype = C.c_int
+        L.nz_mx4_dequantize.argtypes = [pm, sz, sz, vp, C.c_int, sz, vp]
+        L.nz_mx4_dequantize.restype = C.c_int
+        L.nz_mx4_reduce_k.argtypes = [pm, C.c_uint32, vp, sz, sz, sz, C.c_int, C.c_uint32, pm, vp]
+        L.nz_mx4_reduce_k.restype = C.c_int
+        L.nz_mx4_sum_k.argtypes = [pm, C.c_uint32, vp, sz, sz, sz, vp, C.c_int, sz, vp]
+        L.nz_mx4_sum_k.restype = C.c_int
+        L.nz_mx4_workspace_bytes.argtypes = [C.c_int, C.c_int, sz, sz, sz]
+        L.nz_mx4_workspace_bytes.restype = sz
+        L.nz_mx4_product.argtypes = [pm, pm, sz, sz, sz, vp, C.c_int, sz, vp, sz, vp]
+        L.nz_mx4_product.restype = C.c_int
+        L.nz_mx4_linear.argtypes = [vp, C.c_int, sz, pm, sz, sz, sz, vp, C.c_int, sz, vp, sz, vp]
+        L.nz_mx4_linear.restype = C.c_int
+        L.nz_mx4_grad.argtypes = [vp, C.c_int, sz, pm, sz, sz, sz, vp, C.c_int, sz, vp, sz, vp]
+        L.nz_mx4_grad.restype = C.c_int
         L.nz_trace_events.argtypes = [C.POINTER(C.c_void_p), sz]
         L.nz_trace_events.restype = None
         L.nz_trace_recorded.restype = sz
@@ -231,6 +260,110 @@ def nz_reduce_local_sr(d_in, in_bytes, d_local, d_out, out_cap, n, step, seed, d
     return int(lib().nz_reduce_local_sr(d_in.data_ptr(), in_bytes, d_local.data_ptr(), d_out.data_ptr(), out_cap, n,
                                         C.c_float(step), seed, d_res.data_ptr(), _po(opts), d_ws.data_ptr(), ws_bytes,
                                         _stream(stream)))
+
+
+class Mx4:
+    """A matrix in microscaled 4-bit blocks: uint8 cuda tensors codes [rows, 16 * pitch] and scales [rows, pitch], contiguous."""
+
+    def __init__(self, codes, scales):
+        if (codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2
+                or tuple(codes.shape) != (scales.shape[0], 16 * scales.shape[1]) or not codes.is_contiguous()
+                or not scales.is_contiguous()):
+            raise ValueError("codes [rows, 16 * pitch] and scales [rows, pitch] of uint8 are needed, contiguous")
+        self.codes, self.scales, self.rows = codes, scales, scales.shape[0]
+        self.c = Mx4Matrix(codes.data_ptr(), scales.data_ptr(), scales.shape[1])
+
+    @classmethod
+    def empty(cls, rows, cols, device="cuda:0"):
+        p = nz_mx4_pitch(cols)
+        return cls(torch.empty(rows, 16 * p, dtype=torch.uint8, device=device),
+                   torch.empty(rows, p, dtype=torch.uint8, device=device))
+
+
+def _float_type(t):
+    return _FLOAT_TYPES.get(t.dtype, -1)
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _here(stream, *tensors):
+    """Whether the tensors lie on the current device, and the stream belongs to it."""
+    if any(t is not None and not t.is_cuda for t in tensors):
+        return False
+    dev = torch.cuda.current_device()
+    return all(t is None or t.get_device() == dev for t in tensors) and (stream is None or stream.device_index == dev)
+
+
+def nz_mx4_pitch(cols):
+    return int(lib().nz_mx4_pitch(cols))
+
+
+def nz_mx4_quantize(d_in, rows, cols, ld, rounding, seed, out, stream=None):
+    """d_in: float32, bfloat16 or float16 cuda tensor, ld elements from row to row; out: Mx4.  As every call on an Mx4 below:
+    ERR_INVALID for tensors that do not lie on the current device, and for an Mx4 of fewer rows than the call names."""
+    if out.rows < rows or not _here(stream, d_in, out.codes, out.scales):
+        return ERR_INVALID
+    return int(lib().nz_mx4_quantize(d_in.data_ptr(), _float_type(d_in), rows, cols, ld, rounding, seed, out.c, _stream(stream)))
+
+
+def nz_mx4_dequantize(m, rows, cols, d_out, ld, stream=None):
+    if m.rows < rows or not _here(stream, m.codes, m.scales, d_out):
+        return ERR_INVALID
+    return int(lib().nz_mx4_dequantize(m.c, rows, cols, d_out.data_ptr(), _float_type(d_out), ld, _stream(stream)))
+
+
+def _mx4_operands(ms, rows, d_local, stream, *out):
+    """The host array of a sum's operands, or None where they do not fit."""
+    if any(m.rows < rows for m in ms) or not _here(stream, d_local, *out, *[t for m in ms for t in (m.codes, m.scales)]) or (
+            d_local is not None and d_local.dtype != torch.float32):
+        return None
+    return (Mx4Matrix * max(len(ms), 1))(*[m.c for m in ms])
+
+
+def nz_mx4_reduce_k(ms, d_local, ld_local, rows, cols, rounding, seed, out, stream=None):
+    """ms: sequence of Mx4 (the host array is built here); d_local: float32 cuda tensor or None."""
+    ops = _mx4_operands(ms, rows, d_local, stream, out.codes, out.scales)
+    if ops is None or out.rows < rows:
+        return ERR_INVALID
+    return int(lib().nz_mx4_reduce_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, rounding, seed, out.c, _stream(stream)))
+
+
+def nz_mx4_sum_k(ms, d_local, ld_local, rows, cols, d_out, ld, stream=None):
+    ops = _mx4_operands(ms, rows, d_local, stream, d_out)
+    if ops is None:
+        return ERR_INVALID
+    return int(lib().nz_mx4_sum_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, d_out.data_ptr(), _float_type(d_out), ld,
+                                  _stream(stream)))
+
+
+def nz_mx4_workspace_bytes(kind, left, m, n, k):
+    """left: dtype of the float operand (None for MX4_PRODUCT).  Raises ValueError for sizes that the products refuse."""
+    w = int(lib().nz_mx4_workspace_bytes(kind, F32 if left is None else _FLOAT_TYPES.get(left, -1), m, n, k))
+    if w == C.c_size_t(-1).value:
+        raise ValueError("invalid product")
+    return w
+
+
+def nz_mx4_product(a, b, m, n, k, d_c, ldc, d_ws=None, ws_bytes=0, stream=None):
+    if a.rows < m or b.rows < n or not _here(stream, a.codes, a.scales, b.codes, b.scales, d_c, d_ws):
+        return ERR_INVALID
+    return int(lib().nz_mx4_product(a.c, b.c, m, n, k, d_c.data_ptr(), _float_type(d_c), ldc, _ptr(d_ws), ws_bytes, _stream(stream)))
+
+
+def nz_mx4_linear(d_x, ldx, b, m, n, k, d_c, ldc, d_ws=None, ws_bytes=0, stream=None):
+    if b.rows < n or not _here(stream, d_x, b.codes, b.scales, d_c, d_ws):
+        return ERR_INVALID
+    return int(lib().nz_mx4_linear(d_x.data_ptr(), _float_type(d_x), ldx, b.c, m, n, k, d_c.data_ptr(), _float_type(d_c), ldc,
+                                   _ptr(d_ws), ws_bytes, _stream(stream)))
+
+
+def nz_mx4_grad(d_g, ldg, b, m, n, k, d_da, ldda, d_ws=None, ws_bytes=0, stream=None):
+    if b.rows < n or not _here(stream, d_g, b.codes, b.scales, d_da, d_ws):
+        return ERR_INVALID
+    return int(lib().nz_mx4_grad(d_g.data_ptr(), _float_type(d_g), ldg, b.c, m, n, k, d_da.data_ptr(), _float_type(d_da), ldda,
+                                 _ptr(d_ws), ws_bytes, _stream(stream)))
 
 
 def read_result(d_res):

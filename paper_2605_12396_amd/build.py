@@ -5,7 +5,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnz.so")
-SOURCES = ["nz_api.hip", "nz_compress.hip", "nz_decode.hip", "nz_decode_wide.hip"]
+SOURCES = ["nz_api.hip", "nz_compress.hip", "nz_decode.hip", "nz_decode_wide.hip",
+           "nz_mx4.hip", "nz_mx4_product.hip", "nz_mx4_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 

@@ -1,0 +1,226 @@
+// nz_mx4.hip -- conversion of floats into microscaled 4-bit blocks and back, and sums of several such matrices.
+//
+// A thread holds 8 elements of a block (an octet: 4 bytes of codes), four neighbouring lanes hold the block, and a wave 16 blocks: the
+// block's peak takes two exchanges inside groups of four lanes, and codes leave as whole words.  One pass over the data; all of it is bound
+// by memory.
+#include "nz_mx4.hpp"
+
+namespace nz {
+
+namespace {
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kOctets = 4;                       // octets of a thread, kThreads apart
+
+struct Place { uint64_t row; uint32_t blk, q; bool live; };
+
+// Octet number o of a group of rows: which row, which block of it, which quarter of the block.
+__device__ inline Place place(const MxRows& R, uint32_t o, uint32_t limit) {
+    Place p;
+    const uint32_t b = o >> 2;
+    p.q = o & 3u;
+    p.live = b < limit;
+    if (R.rows == 1) { p.row = 0; p.blk = b; return p; }
+    const uint32_t r = __umulhi(b << 3, R.nb_mul) >> R.nb_shift;         // b / nb
+    p.blk = b - r * R.nb;
+    p.row = (uint64_t)blockIdx.y * R.group + r;
+    return p;
+}
+
+__device__ inline uint32_t blocks_here(const MxRows& R) {
+    const uint64_t left = R.rows - (uint64_t)blockIdx.y * R.group;
+    return (uint32_t)(left < R.group ? left : R.group) * R.nb;
+}
+
+template <int T> __device__ inline float as_float(uint16_t v) {
+    if (T == BF16) return __uint_as_float((uint32_t)v << 16);
+    return (float)__builtin_bit_cast(_Float16, v);
+}
+
+// Eight floats of a row from column c on; those past the row's end are 0.
+template <int T> __device__ inline void load8(const void* in, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, bool wide, float* x) {
+    constexpr uint32_t sz = float_bytes(T);
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + (row * ld + c) * sz;
+    if (wide && c + 8 <= cols) {
+        if (T == F32) {
+            const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+        } else {
+            const uint4 u = reinterpret_cast<const uint4*>(p)[0];
+            const uint32_t w[4] = { u.x, u.y, u.z, u.w };
+            for (int i = 0; i < 4; i++) { x[2 * i] = as_float<T>((uint16_t)w[i]); x[2 * i + 1] = as_float<T>((uint16_t)(w[i] >> 16)); }
+        }
+    } else {
+        for (int i = 0; i < 8; i++) {
+            if (T == F32) x[i] = c + i < cols ? reinterpret_cast<const float*>(p)[i] : 0.0f;
+            else x[i] = c + i < cols ? as_float<T>(reinterpret_cast<const uint16_t*>(p)[i]) : 0.0f;
+        }
+    }
+}
+
+template <int T> __device__ inline uint32_t to16(float v) {
+    if (T == BF16) return __builtin_bit_cast(uint16_t, (__bf16)v);
+    return __builtin_bit_cast(uint16_t, (_Float16)v);
+}
+
+template <int T> __device__ inline void store8(void* out, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, bool wide, const float* x) {
+    constexpr uint32_t sz = float_bytes(T);
+    uint8_t* p = reinterpret_cast<uint8_t*>(out) + (row * ld + c) * sz;
+    if (wide && c + 8 <= cols) {
+        if (T == F32) {
+            reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+            uint32_t w[4];
+            for (int i = 0; i < 4; i++) w[i] = to16<T>(x[2 * i]) | to16<T>(x[2 * i + 1]) << 16;
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    } else {
+        for (int i = 0; i < 8; i++)
+            if (c + i < cols) {
+                if (T == F32) reinterpret_cast<float*>(p)[i] = x[i];
+                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)to16<T>(x[i]);
+            }
+    }
+}
+
+// The largest of four neighbouring lanes' values.
+__device__ inline uint32_t max_of_four(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
+}
+
+// One element, stochastically: its code, given its magnitude in units of the block's scale (at most 8, a float without error) and a draw of
+// 16 bits.  Above 1 the grid is that of a float with one bit of mantissa, so the code is the top of the float's own bits and the share of
+// the distance the 22 bits below; under 1 the spacing is 1/2 like that of the octave from 1 on, and 1 is added first, with what this
+// addition rounded away (`rest`) settling a tie.  Adding 2^22 - 33 - 64 u to the bits carries exactly where (u + 1/2) / 2^16 < share.
+__device__ inline uint32_t stochastic_code(float a, uint32_t u) {
+    const float one = a < 1.0f ? 1.0f : 0.0f;
+    const float t = a + one;
+    const uint32_t rest = a > t - one ? 1u : 0u;
+    const uint32_t v = (__float_as_uint(t) + (0x3FFFDFu - (u << 6)) + rest) >> 22;
+    return min(v - (a < 1.0f ? 254u : 252u), 7u);
+}
+
+// Eight elements into a word of codes; the block's scale byte comes back in s.  e: the octet's number, for the draws.
+template <bool SR> __device__ inline uint32_t encode8(const float* x, uint64_t e, uint32_t seed, uint32_t& s) {
+    uint32_t peak = 0;
+    for (int i = 0; i < 8; i++) peak = max(peak, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    peak = max_of_four(peak);
+    const uint32_t ex = peak >> 23;
+    int b = (int)ex - 2;
+    if (SR) b += (peak & 0x7FFFFFu) > 0x400000u ? 1 : 0;
+    b = min(max(b, 0), 252);
+    const bool bad = ex == 255u;
+    uint32_t w = 0;
+    if (!SR) {
+        const float sc = mx_scale((uint32_t)b);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], sc, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], sc, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], sc, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], sc, 3);
+    } else {
+        const float inv = __uint_as_float((uint32_t)(254 - b) << 23);        // 2^(127 - b): exact, and so is the product with it
+        const uint64_t pair = e * 4;
+        const uint32_t key = sr_key(seed, pair);
+        for (int i = 0; i < 4; i++) {
+            const uint32_t h = fmix32(((uint32_t)pair + i) ^ key);
+            for (int j = 0; j < 2; j++) {
+                const float v = x[2 * i + j];
+                const uint32_t c = stochastic_code(fabsf(v) * inv, j ? h >> 16 : h & 0xFFFFu);
+                w |= (c | (__float_as_uint(v) >> 31) << 3) << (8 * i + 4 * j);
+            }
+        }
+    }
+    s = bad ? 255u : (uint32_t)b;
+    return bad ? 0u : w;
+}
+
+__device__ inline void decode8(uint32_t w, uint32_t s, float* x) {
+    const float sc = mx_scale(s);
+    f32x2 v;
+    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 0); x[0] = v[0]; x[1] = v[1];
+    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 1); x[2] = v[0]; x[3] = v[1];
+    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 2); x[4] = v[0]; x[5] = v[1];
+    v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 3); x[6] = v[0]; x[7] = v[1];
+}
+
+template <int T, bool SR>
+__global__ __launch_bounds__(kThreads) void k_mx_quantize(MxConvertArgs A) {
+    const uint32_t limit = blocks_here(A.R);
+    const uint32_t first = blockIdx.x * (kThreads * kOctets) + threadIdx.x;
+    Place p[kOctets];
+    float x[kOctets][8];
+    for (uint32_t u = 0; u < kOctets; u++) {
+        p[u] = place(A.R, first + u * kThreads, limit);
+        if (p[u].live) load8<T>(A.in, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, A.wide, x[u]);
+    }
+    for (uint32_t u = 0; u < kOctets; u++) {
+        if (!p[u].live) continue;                     // (all four lanes of a block)
+        uint32_t s;
+        const uint32_t w = encode8<SR>(x[u], (p[u].row * A.R.nb + p[u].blk) * 4 + p[u].q, A.seed, s);
+        const uint64_t at = p[u].row * A.pitch + p[u].blk;
+        *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p[u].q * 4) = w;
+        if (p[u].q == 0) A.scales[at] = (uint8_t)s;
+    }
+}
+
+// OUT: the floats' type, or -1 for four bits.
+template <int OUT, bool SR>
+__global__ __launch_bounds__(kThreads) void k_mx_sum(MxSumArgs A) {
+    const uint32_t limit = blocks_here(A.R);
+    const Place p = place(A.R, blockIdx.x * kThreads + threadIdx.x, limit);
+    if (!p.live) return;
+    const uint64_t c = p.blk * 32ull + p.q * 8u;
+    float acc[8], x[8];
+    for (uint32_t i = 0; i < A.k; i++) {
+        const uint64_t at = p.row * A.in[i].pitch + p.blk;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(A.in[i].codes + at * 16 + p.q * 4);
+        decode8(w, A.in[i].scales[at], x);
+        for (int j = 0; j < 8; j++) acc[j] = i ? acc[j] + x[j] : x[j];
+    }
+    if (A.local) {
+        load8<F32>(A.local, p.row, A.ld_local, c, A.R.cols, A.local_wide, x);
+        for (int j = 0; j < 8; j++) acc[j] += x[j];
+    }
+    if (OUT >= 0) {
+        store8<OUT < 0 ? F32 : OUT>(A.out, p.row, A.ld, c, A.R.cols, A.wide, acc);
+    } else {
+        uint32_t s;
+        const uint32_t w = encode8<SR>(acc, (p.row * A.R.nb + p.blk) * 4 + p.q, A.seed, s);
+        const uint64_t at = p.row * A.pitch + p.blk;
+        *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p.q * 4) = w;
+        if (p.q == 0) A.scales[at] = (uint8_t)s;
+    }
+}
+
+dim3 grid_of(const MxRows& R, uint32_t octets) {
+    const uint64_t rows = R.rows < R.group ? R.rows : R.group;
+    return dim3((uint32_t)((rows * R.nb * 4 + kThreads * octets - 1) / (kThreads * octets)), (uint32_t)((R.rows + R.group - 1) / R.group));
+}
+
+template <int T> void quantize_type(const MxConvertArgs& A, bool sr, hipStream_t st) {
+    if (sr) hipLaunchKernelGGL((k_mx_quantize<T, true>), grid_of(A.R, kOctets), dim3(kThreads), 0, st, A);
+    else hipLaunchKernelGGL((k_mx_quantize<T, false>), grid_of(A.R, kOctets), dim3(kThreads), 0, st, A);
+}
+
+}  // namespace
+
+hipError_t launch_mx_quantize(const MxConvertArgs& A, int type, bool sr, hipStream_t st) {
+    if (type == F32) quantize_type<F32>(A, sr, st);
+    else if (type == BF16) quantize_type<BF16>(A, sr, st);
+    else quantize_type<F16>(A, sr, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_mx_sum(const MxSumArgs& A, int type, bool sr, hipStream_t st) {
+    const dim3 g = grid_of(A.R, 1), t(kThreads);
+    if (type == F32) hipLaunchKernelGGL((k_mx_sum<F32, false>), g, t, 0, st, A);
+    else if (type == BF16) hipLaunchKernelGGL((k_mx_sum<BF16, false>), g, t, 0, st, A);
+    else if (type == F16) hipLaunchKernelGGL((k_mx_sum<F16, false>), g, t, 0, st, A);
+    else if (sr) hipLaunchKernelGGL((k_mx_sum<-1, true>), g, t, 0, st, A);
+    else hipLaunchKernelGGL((k_mx_sum<-1, false>), g, t, 0, st, A);
+    return hipGetLastError();
+}
+
+}  // namespace nz
