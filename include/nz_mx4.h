@@ -9,8 +9,8 @@
  *           half for even j.  A code is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 2..0).
  *   scales  one byte s at scales + r * pitch + i: the block's elements are its codes times 2^(s - 127); s = 255: all are NaN.
  * `pitch` counts blocks, is a multiple of 4 and at least ceil(cols / 32).  Elements of a last block past `cols` have code 0
- * (nz_mx4_quantize and nz_mx4_reduce_k write them so, and the products count on it); blocks past the last one of a row are
- * neither read for their value nor written.  A message is a matrix of one row.
+ * (nz_mx4_quantize and nz_mx4_reduce_k write them so, and the products count on it).  The buffers hold rows * pitch blocks;
+ * those past the last one of a row are not written, and their contents do not matter.  A message is a matrix of one row.
  *
  * Conventions are those of nz.h: device pointers 16-byte aligned (codes, scales, floats, workspace), the caller owns every
  * buffer, nothing is allocated, no state is kept, kernels are enqueued on `stream` (of the current device) and never
