@@ -55,7 +55,7 @@ hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStre
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// 2^(s - 127) as the conversion and matrix instructions take a scale: the exponent bits alone, NaN for 255.
-__device__ inline float mx_scale(uint32_t s) { return __uint_as_float(s == 255u ? 0x7FC00000u : s == 0u ? 0x00400000u : s << 23); }
+// 2^(s - 127) as the conversion instructions take a scale: they read the exponent bits alone, 0 as 2^-127 and 255 as NaN.
+__device__ inline float mx_scale(uint32_t s) { return __uint_as_float(s << 23); }
 
 }  // namespace nz

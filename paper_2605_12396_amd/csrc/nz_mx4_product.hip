@@ -23,6 +23,16 @@ constexpr uint32_t kNowhere = 0x80000000u;        // an offset behind every buff
 __device__ inline rsrc_t buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00027000); }
 __device__ inline i32x4 load16(rsrc_t r, uint32_t off) { return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0)); }
 
+template <int BYTES> __device__ inline void load_lds(rsrc_t r, uint8_t* to, uint32_t off) {       // to: of the wave's first lane
+    typedef __attribute__((address_space(3))) void* lds_t;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t)to, 16, off, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t)to, 4, off, 0, 0, 0);
+}
+
+template <typename F> __device__ __forceinline__ void unroll4(F f) {
+    f(std::integral_constant<int, 0>{}); f(std::integral_constant<int, 1>{}); f(std::integral_constant<int, 2>{}); f(std::integral_constant<int, 3>{});
+}
+
 struct TileArgs {
     const uint8_t* left; uint64_t left_pitch;             // bytes of a row
     const uint8_t* left_scales; uint64_t left_spitch;     // product
@@ -34,12 +44,6 @@ struct TileArgs {
     uint32_t tiles_m, tiles_j;
     void* c; uint64_t ldc; int c_type;
 };
-
-__device__ inline void store_c(const TileArgs& A, uint64_t at, float v) {
-    if (A.c_type == F32) reinterpret_cast<float*>(A.c)[at] = v;
-    else if (A.c_type == BF16) reinterpret_cast<__bf16*>(A.c)[at] = (__bf16)v;
-    else reinterpret_cast<_Float16*>(A.c)[at] = (_Float16)v;
-}
 
 // Which tile: neighbouring workgroups go to the 8 XCDs in turn, so each XCD is given a contiguous run of tiles; in it, bands of 8 tiles of
 // m are walked along j, so that the 32 tiles that an XCD works on at a time share a few panels of either side in its L2.
@@ -53,195 +57,269 @@ __device__ inline void tile_of(const TileArgs& A, uint32_t& tm, uint32_t& tj) {
     tj = in / height;
 }
 
-// A tile of BM x BN elements of C by four waves, each a quarter of it in tiles of 32 x 32.  A step covers 128 bytes of every row of the
-// left: 256 elements in four bits, 64 in bf16.  While a step is multiplied from one half of the shared memory, the next one is on its way
-// to registers, and is written to the other half at the step's end.
-// Rows lie in shared memory as 8 chunks of 16 bytes, chunk c of row r at c ^ (r ^ r / 8) % 8, so that 8 lanes that read the same chunk of 8
-// rows (and, in the gradient, 8 that write the same chunk of every eighth row) use all banks.
+// A tile of BM x BN elements of C by WM x WN waves, each in tiles of 32 x 32.  A step covers 128 bytes of every row of the left: 256
+// elements in four bits, 64 in bf16.  While a step is multiplied from one half of the shared memory, the next one is on its way to the other.
+// Rows lie in shared memory as 8 chunks of 16 bytes, chunk c of row r at c ^ r % 8, so that 8 lanes that read the same chunk of 8 rows use
+// all banks; chunks are exchanged where they are loaded from, since a wave's direct loads fill shared memory in the order of its lanes.
 // A lane of group g = lane / 32 takes block 4 g + j of a row (product) or elements 32 g + 8 j .. + 7 (linear, grad) in its j-th matrix
 // instruction; which elements meet in one instruction does not matter as long as both sides agree.
-template <int OP, int BM, int BN>
-__global__ __launch_bounds__(256, 1) void k_mx_tile(TileArgs A) {
-    constexpr int TM = BM / 64, TN = BN / 64;
-    constexpr int LL = BM / 32;                                        // 16-byte loads of the left by a thread
-    constexpr int RL = OP == PRODUCT ? BN / 32 : BN / 128;             // of the right (grad: see below)
-    constexpr uint32_t RB = OP == LINEAR ? 32 : 128;                   // bytes of a row of the right in shared memory
-    constexpr int GC = BN / 32;                                        // grad: columns of a thread's piece, 8 rows deep
-    constexpr uint32_t SB = OP == PRODUCT ? 8 : OP == LINEAR ? 2 : 0;  // scales of a row and step
-    __shared__ __attribute__((aligned(16))) uint8_t sl[2][BM * 128];
-    __shared__ __attribute__((aligned(16))) uint8_t sr[2][BN * RB];
-    __shared__ __attribute__((aligned(16))) uint8_t ssl[2][OP == PRODUCT ? BM * 8 : 16];
-    __shared__ __attribute__((aligned(16))) uint8_t ssr[2][SB ? BN * SB : 16];
+template <int OP, int BM, int BN, int WM, int WN> struct Tile {
+    static constexpr uint32_t NT = 64 * WM * WN;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+    static constexpr uint32_t RB = OP == LINEAR ? 32 : 128;            // bytes of a row of the right in shared memory
+    static constexpr int LL = BM * 8 / NT, RL = OP == GRAD ? 0 : BN * (RB / 16) / NT;      // 16-byte loads of a thread
+    static constexpr int SL = OP == PRODUCT ? BM * 2 / NT : 0;                             // 4-byte loads of scales
+    static constexpr int SR = OP == PRODUCT ? BN * 2 / NT : OP == LINEAR ? (BN + NT - 1) / NT : 0;
+    static constexpr uint32_t PW = BN * 32 / NT;                       // grad: columns of a thread's piece, two rows deep
 
-    uint32_t tm, tj;
-    tile_of(A, tm, tj);
-    const uint64_t m0 = (uint64_t)tm * BM, j0 = (uint64_t)tj * BN;
-    const uint32_t t = threadIdx.x, lane = t % 64, wave = t / 64;
-    const uint32_t rows = (uint32_t)min(A.M - m0, (uint64_t)BM), cols = (uint32_t)min(A.outer - j0, (uint64_t)BN);
-    const uint32_t nb = (uint32_t)((A.inner + 31) / 32);
-
-    // ---- where a thread's loads come from: rows past the end read the last one, and are not stored ----
-    const uint8_t* const left = A.left + m0 * A.left_pitch;
-    uint32_t lo[LL];
-    for (int i = 0; i < LL; i++) lo[i] = min(t / 8 + 32 * i, rows - 1) * (uint32_t)A.left_pitch + t % 8 * 16;
-    const uint8_t* const right = OP == GRAD ? A.right + j0 / 2 : A.right + j0 * A.right_pitch;
-    uint32_t ro[RL < 1 ? 1 : RL];
-    if (OP == PRODUCT) for (int i = 0; i < RL; i++) ro[i] = min(t / 8 + 32 * i, cols - 1) * (uint32_t)A.right_pitch + t % 8 * 16;
-    if (OP == LINEAR) for (int i = 0; i < RL; i++) ro[i] = min(t / 2 + 128 * i, cols - 1) * (uint32_t)A.right_pitch + t % 2 * 16;
-    const uint32_t deep = t / 32, across = t % 32;                     // grad: rows 8 deep .. + 7, columns GC across .. + GC - 1
-    const bool inside = OP != GRAD || across * GC < (uint32_t)((A.outer + 31) / 32 * 32 - j0);
-
-    i32x4 lv[LL], rv[RL < 1 ? 1 : RL];
-    uint32_t gw[8], gs[8];
-    uint64_t slv = 0, srv = 0;
-
-    auto fetch = [&](uint32_t s) {
-        const uint32_t rs = OP == PRODUCT ? s : s / A.terms;           // step of the right
-        const rsrc_t bl = buffer_at(left + (uint64_t)s * 128);
-        const bool l_in = OP == PRODUCT ? s * 8 + t % 8 < nb : A.terms > 1 || (uint64_t)rs * 64 + t % 8 * 8 < A.inner;
-        for (int i = 0; i < LL; i++) lv[i] = load16(bl, l_in ? lo[i] : kNowhere);
-        if (OP == PRODUCT) {
-            const rsrc_t br = buffer_at(right + (uint64_t)s * 128);
-            for (int i = 0; i < RL; i++) rv[i] = load16(br, l_in ? ro[i] : kNowhere);
-            // scales: a thread's row of either side, 8 blocks; those past the row's end become 0 (the codes there are 0)
-            const rsrc_t sl_ = buffer_at(A.left_scales + m0 * A.left_spitch + (uint64_t)s * 8);
-            const rsrc_t sr_ = buffer_at(A.right_scales + j0 * A.right_spitch + (uint64_t)s * 8);
-            const uint32_t left_here = nb - s * 8;
-            const uint32_t a = min(t % BM, rows - 1) * (uint32_t)A.left_spitch, b = min(t % BN, cols - 1) * (uint32_t)A.right_spitch;
-            const uint32_t hi_in = left_here > 4 ? 4u : kNowhere;
-            const uint32_t a0 = __builtin_amdgcn_raw_buffer_load_b32(sl_, a, 0, 0), a1 = __builtin_amdgcn_raw_buffer_load_b32(sl_, hi_in == 4u ? a + 4 : kNowhere, 0, 0);
-            const uint32_t b0 = __builtin_amdgcn_raw_buffer_load_b32(sr_, b, 0, 0), b1 = __builtin_amdgcn_raw_buffer_load_b32(sr_, hi_in == 4u ? b + 4 : kNowhere, 0, 0);
-            const uint64_t keep = left_here >= 8 ? ~0ull : (1ull << (8 * left_here)) - 1;
-            slv = ((uint64_t)a1 << 32 | a0) & keep;
-            srv = ((uint64_t)b1 << 32 | b0) & keep;
-        } else if (OP == LINEAR) {
-            const rsrc_t br = buffer_at(right + (uint64_t)rs * 32);
-            const bool r_in = rs * 2 + t % 2 < nb;
-            for (int i = 0; i < RL; i++) rv[i] = load16(br, r_in ? ro[i] : kNowhere);
-            const rsrc_t sr_ = buffer_at(A.right_scales + j0 * A.right_spitch + (uint64_t)rs * 2);
-            const uint32_t b = __builtin_amdgcn_raw_buffer_load_b16(sr_, min(t % BN, cols - 1) * (uint32_t)A.right_spitch, 0, 0);
-            srv = rs * 2 + 1 < nb ? b : b & 0xFFu;
-        } else {
-            const rsrc_t br = buffer_at(right + (uint64_t)rs * 64 * A.right_pitch);
-            const rsrc_t sr_ = buffer_at(A.right_scales + j0 / 32 + (uint64_t)rs * 64 * A.right_spitch);
-            for (int r = 0; r < 8; r++) {
-                const uint32_t row = deep * 8 + r;
-                const bool in = inside && (uint64_t)rs * 64 + row < A.inner;
-                const uint32_t off = in ? row * (uint32_t)A.right_pitch + across * (GC / 2) : kNowhere;
-                gw[r] = GC == 8 ? __builtin_amdgcn_raw_buffer_load_b32(br, off, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(br, off, 0, 0);
-                gs[r] = __builtin_amdgcn_raw_buffer_load_b8(sr_, in ? row * (uint32_t)A.right_spitch + across * GC / 32 : kNowhere, 0, 0);
-            }
-        }
+    struct Half {
+        uint8_t l[BM * 128];
+        uint8_t r[BN * RB];
+        uint8_t sl[OP == PRODUCT ? BM * 8 : 16];
+        uint8_t sr[OP == PRODUCT ? BN * 8 : OP == LINEAR ? BN * 4 : 16];
     };
 
-    auto swz = [](uint32_t row, uint32_t chunk) { return row * 128 + (chunk ^ ((row ^ row >> 3) & 7)) * 16; };
+    // What stays the same from step to step.  Rows past the end read the last one, and are not stored.
+    const TileArgs& A;
+    uint32_t t, lane, wave, g, l32, wm, wj, rows, cols, nb;
+    uint64_t m0, j0;
+    const uint8_t *left, *right, *left_s, *right_s;
+    uint32_t lo[LL], ro[RL ? RL : 1], slo[SL ? SL : 1], sro[SR ? SR : 1];
+    uint32_t lchunk;
+    uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1, columns PW gq .. of a piece
+    i32x4 gw[2];
+    uint32_t gs[2];
 
-    auto put = [&](int h) {
-        for (int i = 0; i < LL; i++) *reinterpret_cast<i32x4*>(&sl[h][swz(t / 8 + 32 * i, t % 8)]) = lv[i];
-        if (OP == PRODUCT) {
-            for (int i = 0; i < RL; i++) *reinterpret_cast<i32x4*>(&sr[h][swz(t / 8 + 32 * i, t % 8)]) = rv[i];
-            if (t < BM) *reinterpret_cast<uint64_t*>(&ssl[h][t * 8]) = slv;
-            if (t < BN) *reinterpret_cast<uint64_t*>(&ssr[h][t * 8]) = srv;
-        } else if (OP == LINEAR) {
-            for (int i = 0; i < RL; i++) *reinterpret_cast<i32x4*>(&sr[h][(t / 2 + 128 * i) * 32 + t % 2 * 16]) = rv[i];
-            if (t < BN) *reinterpret_cast<uint16_t*>(&ssr[h][t * 2]) = (uint16_t)srv;
-        } else {
-            // 8 rows x GC columns of codes become GC rows x 8 of bf16
-            uint32_t p[8][GC / 2];
-            for (int r = 0; r < 8; r++) {
-                const float sc = mx_scale(gs[r]);
-                p[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[r], sc, 0));
-                p[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[r], sc, 1));
-                if constexpr (GC == 8) {
-                    p[r][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[r], sc, 2));
-                    p[r][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[r], sc, 3));
-                }
-            }
-            for (int c = 0; c < GC; c++) {
-                i32x4 v;
-                for (int d = 0; d < 4; d++)
-                    v[d] = c & 1 ? __builtin_amdgcn_perm(p[2 * d + 1][c / 2], p[2 * d][c / 2], 0x07060302u)
-                                 : __builtin_amdgcn_perm(p[2 * d + 1][c / 2], p[2 * d][c / 2], 0x05040100u);
-                *reinterpret_cast<i32x4*>(&sr[h][swz(across * GC + c, deep)]) = v;
-            }
-        }
-    };
-
-    f32x16 acc[TM][TN];
+    __device__ __forceinline__ explicit Tile(const TileArgs& args) : A(args) {
+        uint32_t tm, tj;
+        tile_of(A, tm, tj);
+        tm = __builtin_amdgcn_readfirstlane(tm); tj = __builtin_amdgcn_readfirstlane(tj);      // (the same in all lanes anyway)
+        m0 = (uint64_t)tm * BM; j0 = (uint64_t)tj * BN;
+        t = threadIdx.x; lane = t % 64; wave = __builtin_amdgcn_readfirstlane(t / 64);
+        g = lane / 32; l32 = lane % 32;
+        wm = wave / WN * (BM / WM); wj = wave % WN * (BN / WN);
+        rows = (uint32_t)min(A.M - m0, (uint64_t)BM); cols = (uint32_t)min(A.outer - j0, (uint64_t)BN);
+        nb = (uint32_t)((A.inner + 31) / 32);
+        left = A.left + m0 * A.left_pitch;
+        right = OP == GRAD ? A.right + j0 / 2 : A.right + j0 * A.right_pitch;
+        left_s = A.left_scales + m0 * A.left_spitch;
+        right_s = OP == GRAD ? A.right_scales + j0 / 32 : A.right_scales + j0 * A.right_spitch;
+        lchunk = t % 8 ^ t / 8 % 8;
 #pragma unroll
-    for (int a = 0; a < TM; a++)
+        for (int i = 0; i < LL; i++) lo[i] = min(t / 8 + NT / 8 * i, rows - 1) * (uint32_t)A.left_pitch + lchunk * 16;
 #pragma unroll
-        for (int b = 0; b < TN; b++) acc[a][b] = f32x16{};
-    const uint32_t g = lane / 32, l32 = lane % 32;
-    const uint32_t wm = wave / 2 * (BM / 2), wj = wave % 2 * (BN / 2);
-
-    auto multiply = [&](int h) {
-        if constexpr (OP == PRODUCT) {
-            int sa[TM], sb[TN];
-            for (int a = 0; a < TM; a++) sa[a] = *reinterpret_cast<const int*>(&ssl[h][(wm + a * 32 + l32) * 8 + g * 4]);
-            for (int b = 0; b < TN; b++) sb[b] = *reinterpret_cast<const int*>(&ssr[h][(wj + b * 32 + l32) * 8 + g * 4]);
-            auto block = [&](auto J) {
-                constexpr int j = decltype(J)::value;
-                i32x4 x[TM], y[TN];
-                for (int a = 0; a < TM; a++) x[a] = *reinterpret_cast<const i32x4*>(&sl[h][swz(wm + a * 32 + l32, g * 4 + j)]);
-                for (int b = 0; b < TN; b++) y[b] = *reinterpret_cast<const i32x4*>(&sr[h][swz(wj + b * 32 + l32, g * 4 + j)]);
-                for (int a = 0; a < TM; a++)
-                    for (int b = 0; b < TN; b++) {
-                        const i32x8 xa = { x[a][0], x[a][1], x[a][2], x[a][3], 0, 0, 0, 0 }, yb = { y[b][0], y[b][1], y[b][2], y[b][3], 0, 0, 0, 0 };
-                        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xa, yb, acc[a][b], 4, 4, j, sa[a], j, sb[b]);
-                    }
-            };
-            block(std::integral_constant<int, 0>{}); block(std::integral_constant<int, 1>{});
-            block(std::integral_constant<int, 2>{}); block(std::integral_constant<int, 3>{});
-        } else {
-            i32x4 w[TN];
-            float sc[TN];
-            if (OP == LINEAR)
-                for (int b = 0; b < TN; b++) {
-                    w[b] = *reinterpret_cast<const i32x4*>(&sr[h][(wj + b * 32 + l32) * 32 + g * 16]);
-                    sc[b] = mx_scale(ssr[h][(wj + b * 32 + l32) * 2 + g]);
-                }
-            for (int j = 0; j < 4; j++) {
-                bf16x8 x[TM], y[TN];
-                for (int a = 0; a < TM; a++) x[a] = *reinterpret_cast<const bf16x8*>(&sl[h][swz(wm + a * 32 + l32, g * 4 + j)]);
-                for (int b = 0; b < TN; b++) {
-                    if (OP == GRAD) {
-                        y[b] = *reinterpret_cast<const bf16x8*>(&sr[h][swz(wj + b * 32 + l32, g * 4 + j)]);
-                    } else {
-                        i32x4 v;
-                        v[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[b][j], sc[b], 0));
-                        v[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[b][j], sc[b], 1));
-                        v[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[b][j], sc[b], 2));
-                        v[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[b][j], sc[b], 3));
-                        y[b] = __builtin_bit_cast(bf16x8, v);
-                    }
-                }
-                for (int a = 0; a < TM; a++)
-                    for (int b = 0; b < TN; b++) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[a], y[b], acc[a][b], 0, 0, 0);
-            }
-        }
-    };
-
-    fetch(0);
-    put(0);
-    for (uint32_t s = 0; s < A.steps; s++) {
-        __syncthreads();
-        if (s + 1 < A.steps) fetch(s + 1);
-        multiply(s & 1);
-        if (s + 1 < A.steps) put((s + 1) & 1);
+        for (int i = 0; i < RL; i++)
+            ro[i] = OP == PRODUCT ? min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16
+                                  : min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_pitch + t % 2 * 16;
+#pragma unroll
+        for (int i = 0; i < SL; i++) slo[i] = min(t / 2 + NT / 2 * i, rows - 1) * (uint32_t)A.left_spitch + t % 2 * 4;
+#pragma unroll
+        for (int i = 0; i < SR; i++)
+            sro[i] = OP == PRODUCT ? min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_spitch + t % 2 * 4
+                                   : min(t + NT * i, cols - 1) * (uint32_t)A.right_spitch;
+        gd = t % 32; gq = t / 32;
     }
 
+    // Sends for step s.  What lies past the end of a row comes as zeros.
+    __device__ __forceinline__ void fetch(uint32_t s, Half* __restrict h) {
+        const uint32_t rs = OP == PRODUCT ? s : s / A.terms;           // step of the right
+        const rsrc_t bl = buffer_at(left + (uint64_t)s * 128);
+        const bool on = s < A.steps;                                   // (past the last step: nothing is read)
+        const bool l_in = OP == PRODUCT ? s * 8 + lchunk < nb : on && (A.terms > 1 || (uint64_t)rs * 64 + lchunk * 8 < A.inner);
 #pragma unroll
-    for (int a = 0; a < TM; a++)
+        for (int i = 0; i < LL; i++) load_lds<16>(bl, h->l + (i * NT + wave * 64) * 16, l_in ? lo[i] : kNowhere);
+        if (OP == GRAD) {
+            // (a piece of 32 columns is one block; one of 16 half of one)
+            const rsrc_t br = buffer_at(right + (uint64_t)rs * 64 * A.right_pitch), bs = buffer_at(right_s + (uint64_t)rs * 64 * A.right_spitch);
+            const bool c_in = gq * PW < (uint32_t)((A.outer + 31) / 32 * 32 - j0);
 #pragma unroll
-        for (int i = 0; i < 16; i++) {
-            const uint32_t m = wm + a * 32 + i / 4 * 8 + g * 4 + i % 4;
+            for (int r = 0; r < 2; r++) {
+                const uint32_t row = gd * 2 + r;
+                const bool in = on && c_in && (uint64_t)rs * 64 + row < A.inner;
+                const uint32_t off = in ? row * (uint32_t)A.right_pitch + gq * (PW / 2) : kNowhere;
+                if constexpr (PW == 32) gw[r] = load16(br, off);
+                else {
+                    const auto v = __builtin_amdgcn_raw_buffer_load_b64(br, off, 0, 0);
+                    gw[r][0] = v[0]; gw[r][1] = v[1];
+                }
+                gs[r] = __builtin_amdgcn_raw_buffer_load_b8(bs, in ? row * (uint32_t)A.right_spitch + gq * PW / 32 : kNowhere, 0, 0);
+            }
+        } else {
+            const rsrc_t br = buffer_at(right + (uint64_t)rs * RB);
+            const bool r_in = OP == PRODUCT ? l_in : on && rs * 2 + t % 2 < nb;
 #pragma unroll
-            for (int b = 0; b < TN; b++) {
-                const uint32_t j = wj + b * 32 + l32;
-                if (m < rows && j < cols) store_c(A, (m0 + m) * A.ldc + j0 + j, acc[a][b][i]);
+            for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, r_in ? ro[i] : kNowhere);
+            if (OP == PRODUCT) {
+                const rsrc_t bsl = buffer_at(left_s + (uint64_t)s * 8), bsr = buffer_at(right_s + (uint64_t)s * 8);
+                const bool s_in = s * 8 + t % 2 * 4 < nb;
+#pragma unroll
+                for (int i = 0; i < SL; i++) load_lds<4>(bsl, h->sl + (i * NT + wave * 64) * 4, s_in ? slo[i] : kNowhere);
+#pragma unroll
+                for (int i = 0; i < SR; i++) load_lds<4>(bsr, h->sr + (i * NT + wave * 64) * 4, s_in ? sro[i] : kNowhere);
+            } else {
+                const rsrc_t bsr = buffer_at(right_s + (uint64_t)(rs / 2) * 4);     // (the scales of two steps)
+#pragma unroll
+                for (int i = 0; i < SR; i++)
+                    if (BN % NT == 0 || wave * 64 < BN) load_lds<4>(bsr, h->sr + (i * NT + wave * 64) * 4, on ? sro[i] : kNowhere);
             }
         }
+    }
+
+    // grad: two rows of codes become columns of bf16, two rows to a word.
+    __device__ __forceinline__ void turn(Half* __restrict h) {
+        if constexpr (OP == GRAD) {
+            const float s0 = mx_scale(gs[0]), s1 = mx_scale(gs[1]);
+#pragma unroll
+            for (uint32_t w = 0; w < PW / 8; w++)
+                unroll4([&](auto B) {
+                    const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[0][w], s0, B.value));
+                    const uint32_t q = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[1][w], s1, B.value));
+                    const uint32_t col = gq * PW + w * 8 + B.value * 2;
+                    *reinterpret_cast<uint32_t*>(h->r + col * 128 + ((gd / 4 ^ col % 8) * 16) + gd % 4 * 4) = __builtin_amdgcn_perm(q, p, 0x05040100u);
+                    *reinterpret_cast<uint32_t*>(h->r + (col + 1) * 128 + ((gd / 4 ^ (col + 1) % 8) * 16) + gd % 4 * 4) =
+                        __builtin_amdgcn_perm(q, p, 0x07060302u);
+                });
+        }
+    }
+
+    // What a lane multiplies: a fragment of either side for one of a step's four matrix instructions, and what serves all four.
+    struct Frag { i32x4 x[TM], y[TN]; };
+    struct Side { int sl[TM], sr[TN]; i32x4 w[TN]; };
+
+    __device__ __forceinline__ void load_side(uint32_t s, const Half* __restrict h, Side& S) {
+        if constexpr (OP == PRODUCT) {
+            const uint32_t in = nb - min(s * 8 + g * 4, nb);           // blocks of this lane's four that there are
+            const int keep = in >= 4 ? -1 : (1 << 8 * in) - 1;
+#pragma unroll
+            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(h->sl + (wm + a * 32 + l32) * 8 + g * 4) & keep;
+#pragma unroll
+            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(h->sr + (wj + b * 32 + l32) * 8 + g * 4) & keep;
+        }
+        if constexpr (OP == LINEAR) {
+            const uint32_t blk = s / A.terms * 2 + g;
+#pragma unroll
+            for (int b = 0; b < TN; b++) {
+                S.w[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + g * 16);
+                const uint32_t sb = h->sr[(wj + b * 32 + l32) * 4 + blk % 4];
+                S.sr[b] = blk < nb ? sb << 23 : 0;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void load_frag(int j, const Half* __restrict h, Frag& F) {
+        const uint32_t c = ((g * 4 + j) ^ l32 % 8) * 16;
+#pragma unroll
+        for (int a = 0; a < TM; a++) F.x[a] = *reinterpret_cast<const i32x4*>(h->l + (wm + a * 32 + l32) * 128 + c);
+        if constexpr (OP != LINEAR)
+#pragma unroll
+            for (int b = 0; b < TN; b++) F.y[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + c);
+    }
+
+    template <int j> __device__ __forceinline__ void multiply(Frag& F, const Side& S, f32x16 (&acc)[TM][TN]) {
+        if constexpr (OP == LINEAR)
+#pragma unroll
+            for (int b = 0; b < TN; b++)
+                unroll4([&](auto B) {
+                    F.y[b][B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(S.w[b][j], __int_as_float(S.sr[b]), B.value));
+                });
+#pragma unroll
+        for (int a = 0; a < TM; a++)
+#pragma unroll
+            for (int b = 0; b < TN; b++)
+                if constexpr (OP == PRODUCT) {
+                    const i32x8 x = { F.x[a][0], F.x[a][1], F.x[a][2], F.x[a][3], 0, 0, 0, 0 }, y = { F.y[b][0], F.y[b][1], F.y[b][2], F.y[b][3], 0, 0, 0, 0 };
+                    acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[a][b], 4, 4, j, S.sl[a], j, S.sr[b]);
+                } else {
+                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, F.x[a]), __builtin_bit_cast(bf16x8, F.y[b]), acc[a][b], 0, 0, 0);
+                }
+    }
+
+    static __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
+
+    // This wave's loads have arrived and its reads are done, and so are everyone's.
+    static __device__ __forceinline__ void meet() {
+        pin();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        pin();
+    }
+
+    // Step s, whose first fragments are in registers already.  The workgroup meets while the last of its four multiplications is still to
+    // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.
+    __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
+        Frag F1, F2, F3;
+        load_frag(1, cur, F1);
+        pin();
+        multiply<0>(F, S, acc);
+        pin();
+        load_frag(2, cur, F2);
+        pin();
+        multiply<1>(F1, S, acc);
+        pin();
+        load_frag(3, cur, F3);
+        pin();
+        multiply<2>(F2, S, acc);
+        turn(next);
+        meet();
+        fetch(s + 2, cur);
+        Side S1;
+        load_side(s + 1, next, S1);
+        load_frag(0, next, F);
+        multiply<3>(F3, S, acc);
+#pragma unroll
+        for (int i = 0; i < TM * TN; i++) {                            // one matrix instruction, one read, two loads, and so on
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x10, 2, 0);
+        }
+        pin();
+        S = S1;
+    }
+
+    template <typename T> __device__ __forceinline__ void store(const f32x16 (&acc)[TM][TN]) {
+        T* const c = reinterpret_cast<T*>(A.c) + m0 * A.ldc + j0;
+#pragma unroll
+        for (int a = 0; a < TM; a++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const uint32_t m = wm + a * 32 + i / 4 * 8 + g * 4 + i % 4;
+#pragma unroll
+                for (int b = 0; b < TN; b++) {
+                    const uint32_t j = wj + b * 32 + l32;
+                    if (m < rows && j < cols) c[m * A.ldc + j] = (T)acc[a][b][i];
+                }
+            }
+    }
+};
+
+template <int OP, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
+    typedef Tile<OP, BM, BN, WM, WN> Tl;
+    __shared__ __attribute__((aligned(16))) typename Tl::Half h0, h1;
+    Tl T(A);
+    f32x16 acc[Tl::TM][Tl::TN];
+#pragma unroll
+    for (int a = 0; a < Tl::TM; a++)
+#pragma unroll
+        for (int b = 0; b < Tl::TN; b++) acc[a][b] = f32x16{};
+    T.fetch(0, &h0);
+    T.turn(&h0);
+    T.fetch(1, &h1);
+    T.meet();
+    typename Tl::Frag F;
+    typename Tl::Side S;
+    T.load_side(0, &h0, S);
+    T.load_frag(0, &h0, F);
+    uint32_t s = 0;
+    for (; s + 1 < A.steps; s += 2) {
+        T.step(s, &h0, &h1, F, S, acc);
+        T.step(s + 1, &h1, &h0, F, S, acc);
+    }
+    if (s < A.steps) T.step(s, &h0, &h1, F, S, acc);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                   // no load may reach shared memory after the workgroup's end
+    if (A.c_type == F32) T.template store<float>(acc);
+    else if (A.c_type == BF16) T.template store<__bf16>(acc);
+    else T.template store<_Float16>(acc);
 }
 
 // Floats of the left as bf16 terms that add up to them: one for bf16, two for fp16 (11 bits), three for float32 (24 bits).  Each term
@@ -277,13 +355,17 @@ __global__ __launch_bounds__(256) void k_mx_terms(const void* x, uint64_t ldx, u
     for (int q = 0; q < terms; q++) *reinterpret_cast<uint4*>(at + q * 64) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
 }
 
+template <int OP, int BM, int BN, int WM, int WN> void launch_tile(const TileArgs& T, hipStream_t st) {
+    hipLaunchKernelGGL((k_mx_tile<OP, BM, BN, WM, WN>), dim3(T.tiles_m * T.tiles_j), dim3(64 * WM * WN), 0, st, T);
+}
+
 template <int OP> hipError_t launch_tiles(TileArgs& T, hipStream_t st) {
     auto count = [&](uint32_t bm, uint32_t bn) {
         T.tiles_m = (uint32_t)((T.M + bm - 1) / bm); T.tiles_j = (uint32_t)((T.outer + bn - 1) / bn);
         return T.tiles_m * T.tiles_j;
     };
-    if (count(256, 256) >= 192) hipLaunchKernelGGL((k_mx_tile<OP, 256, 256>), dim3(count(256, 256)), dim3(256), 0, st, T);
-    else hipLaunchKernelGGL((k_mx_tile<OP, 128, 128>), dim3(count(128, 128)), dim3(256), 0, st, T);
+    if (count(256, 256) >= 192) launch_tile<OP, 256, 256, 2, 2>(T, st);
+    else { count(128, 128); launch_tile<OP, 128, 128, 2, 2>(T, st); }
     return hipGetLastError();
 }
 

@@ -82,6 +82,27 @@ def test_linear_and_grad_exact(nz, size, left):
         check(nz, nz.MX4_GRAD, floats(nz, g, left, n + pad)[0], bm, m, n, k, out, g @ w, ld_pad=pad)
 
 
+@pytest.mark.parametrize("size", [(3588, 3850, 300), (3841, 4100, 1056)], ids=str)
+def test_sizes_that_fill_the_chip(nz, size):
+    """Large tiles, ragged in every direction, against float64 on the GPU."""
+    import torch
+    m, n, k = size
+    rng = np.random.default_rng(m)
+    a, b = R.random_matrix(rng, m, k, 126, 129), R.random_matrix(rng, n, k, 126, 129)
+    av, w = dev(R.values(*a, k)), dev(R.values(*b, k))
+    bm = mat(nz, *R.place(*b, k))
+    check(nz, nz.MX4_PRODUCT, mat(nz, *R.place(*a, k)), bm, m, n, k, "f32", (av @ w.t()).cpu().numpy(), ld_pad=1)
+    for left in ("bf16", "f16"):
+        x, g = exact_floats(rng, m, k), exact_floats(rng, m, n)
+        check(nz, nz.MX4_LINEAR, floats(nz, x, left, k + 4)[0], bm, m, n, k, "bf16", (dev(x) @ w.t()).cpu().numpy())
+        check(nz, nz.MX4_GRAD, floats(nz, g, left, n + 2)[0], bm, m, n, k, "f16", (dev(g) @ w).cpu().numpy())
+    # and the widest of the gradient: as many columns of B as make large tiles there
+    n, k = k, n
+    b = R.random_matrix(rng, n, k, 126, 129)
+    g = exact_floats(rng, m, n)
+    check(nz, nz.MX4_GRAD, floats(nz, g, "bf16", (n + 7) // 8 * 8)[0], mat(nz, *R.place(*b, k)), m, n, k, "f32", (dev(g) @ dev(R.values(*b, k))).cpu().numpy())
+
+
 @pytest.mark.parametrize("left", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("size", [(1, 300, 2000), (7, 513, 900), (40, 200, 1500), (130, 700, 260), (600, 300, 515)], ids=str)
 def test_linear_and_grad_of_full_mantissas(nz, size, left):
