@@ -39,7 +39,7 @@ struct TileArgs {
     const uint8_t* right; uint64_t right_pitch;
     const uint8_t* right_scales; uint64_t right_spitch;
     uint64_t M, outer, inner;
-    uint32_t terms;                                       // linear, grad: bf16 terms of a float
+    uint32_t terms, per_term;                             // linear, grad: bf16 terms of a float; 2^31 over that, upwards
     uint32_t steps;                                       // terms counted
     uint32_t tiles_m, tiles_j;
     void* c; uint64_t ldc; int c_type;
@@ -59,8 +59,8 @@ __device__ inline void tile_of(const TileArgs& A, uint32_t& tm, uint32_t& tj) {
 
 // A tile of BM x BN elements of C by WM x WN waves, each in tiles of 32 x 32.  A step covers 128 bytes of every row of the left: 256
 // elements in four bits, 64 in bf16.  While a step is multiplied from one half of the shared memory, the next one is on its way to the other.
-// Rows lie in shared memory as 8 chunks of 16 bytes, chunk c of row r at c ^ r % 8, so that 8 lanes that read the same chunk of 8 rows use
-// all banks; chunks are exchanged where they are loaded from, since a wave's direct loads fill shared memory in the order of its lanes.
+// Rows lie in shared memory as 8 chunks of 16 bytes, chunk c of row r at c ^ r / 2 % 8, so that 16 lanes that read the same chunk of 16 rows
+// use all 64 banks; chunks are exchanged where they are loaded from, since a wave's direct loads fill shared memory in the order of its lanes.
 // A lane of group g = lane / 32 takes block 4 g + j of a row (product) or elements 32 g + 8 j .. + 7 (linear, grad) in its j-th matrix
 // instruction; which elements meet in one instruction does not matter as long as both sides agree.
 template <int OP, int BM, int BN, int WM, int WN> struct Tile {
@@ -78,6 +78,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         uint8_t sl[OP == PRODUCT ? BM * 8 : 16];
         uint8_t sr[OP == PRODUCT ? BN * 8 : OP == LINEAR ? BN * 4 : 16];
     };
+
+    // Results leave through a half's memory: 32 rows of as many columns as it has room for from every wave.  Bytes of such a row, with 16
+    // more that spread the rows over the banks; columns in tiles of 32.
+    static constexpr uint32_t out_bytes(int tiles, uint32_t size) { return tiles * 32 * size + 16; }
+    static constexpr int out_tiles(uint32_t size) {
+        int n = TN;
+        while (32 * out_bytes(n, size) * WM * WN > sizeof(Half)) n /= 2;
+        return n;
+    }
 
     // What stays the same from step to step.  Rows past the end read the last one, and are not stored.
     const TileArgs& A;
@@ -104,13 +113,13 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         right = OP == GRAD ? A.right + j0 / 2 : A.right + j0 * A.right_pitch;
         left_s = A.left_scales + m0 * A.left_spitch;
         right_s = OP == GRAD ? A.right_scales + j0 / 32 : A.right_scales + j0 * A.right_spitch;
-        lchunk = t % 8 ^ t / 8 % 8;
+        lchunk = t % 8 ^ t / 16 % 8;
 #pragma unroll
         for (int i = 0; i < LL; i++) lo[i] = min(t / 8 + NT / 8 * i, rows - 1) * (uint32_t)A.left_pitch + lchunk * 16;
 #pragma unroll
         for (int i = 0; i < RL; i++)
             ro[i] = OP == PRODUCT ? min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16
-                                  : min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_pitch + t % 2 * 16;
+                                  : min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_pitch + (t % 2 ^ t / 16 % 2) * 16;
 #pragma unroll
         for (int i = 0; i < SL; i++) slo[i] = min(t / 2 + NT / 2 * i, rows - 1) * (uint32_t)A.left_spitch + t % 2 * 4;
 #pragma unroll
@@ -120,14 +129,19 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         gd = t % 32; gq = t / 32;
     }
 
-    // Sends for step s.  What lies past the end of a row comes as zeros.
+    // Step s of the left belongs to this step of the right.
+    __device__ __forceinline__ uint32_t right_step(uint32_t s) const {
+        return OP == PRODUCT ? s : __umulhi(2 * s, A.per_term);
+    }
+
+    // Sends for step s: the left (grad: all), and the rest.  What lies past the end of a row comes as zeros, and all of a step past the last.
     __device__ __forceinline__ void fetch(uint32_t s, Half* __restrict h) {
-        const uint32_t rs = OP == PRODUCT ? s : s / A.terms;           // step of the right
+        const uint32_t rs = right_step(s);
         const rsrc_t bl = buffer_at(left + (uint64_t)s * 128);
-        const bool on = s < A.steps;                                   // (past the last step: nothing is read)
-        const bool l_in = OP == PRODUCT ? s * 8 + lchunk < nb : on && (A.terms > 1 || (uint64_t)rs * 64 + lchunk * 8 < A.inner);
+        const bool on = s < A.steps;
+        const bool in = OP == PRODUCT ? s * 8 + lchunk < nb : on & ((A.terms > 1) | ((uint64_t)rs * 64 + lchunk * 8 < A.inner));
 #pragma unroll
-        for (int i = 0; i < LL; i++) load_lds<16>(bl, h->l + (i * NT + wave * 64) * 16, l_in ? lo[i] : kNowhere);
+        for (int i = 0; i < LL; i++) load_lds<16>(bl, h->l + (i * NT + wave * 64) * 16, in ? lo[i] : kNowhere);
         if (OP == GRAD) {
             // (a piece of 32 columns is one block; one of 16 half of one)
             const rsrc_t br = buffer_at(right + (uint64_t)rs * 64 * A.right_pitch), bs = buffer_at(right_s + (uint64_t)rs * 64 * A.right_spitch);
@@ -135,7 +149,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 #pragma unroll
             for (int r = 0; r < 2; r++) {
                 const uint32_t row = gd * 2 + r;
-                const bool in = on && c_in && (uint64_t)rs * 64 + row < A.inner;
+                const bool in = on & c_in & ((uint64_t)rs * 64 + row < A.inner);
                 const uint32_t off = in ? row * (uint32_t)A.right_pitch + gq * (PW / 2) : kNowhere;
                 if constexpr (PW == 32) gw[r] = load16(br, off);
                 else {
@@ -144,9 +158,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
                 }
                 gs[r] = __builtin_amdgcn_raw_buffer_load_b8(bs, in ? row * (uint32_t)A.right_spitch + gq * PW / 32 : kNowhere, 0, 0);
             }
-        } else {
+        }
+    }
+
+    __device__ __forceinline__ void fetch_rest(uint32_t s, Half* __restrict h) {
+        if constexpr (OP != GRAD) {
+            const uint32_t rs = right_step(s);
+            const bool on = s < A.steps;
             const rsrc_t br = buffer_at(right + (uint64_t)rs * RB);
-            const bool r_in = OP == PRODUCT ? l_in : on && rs * 2 + t % 2 < nb;
+            const bool r_in = OP == PRODUCT ? s * 8 + lchunk < nb : on & (rs * 2 + (t % 2 ^ t / 16 % 2) < nb);
 #pragma unroll
             for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, r_in ? ro[i] : kNowhere);
             if (OP == PRODUCT) {
@@ -175,8 +195,8 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
                     const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[0][w], s0, B.value));
                     const uint32_t q = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[1][w], s1, B.value));
                     const uint32_t col = gq * PW + w * 8 + B.value * 2;
-                    *reinterpret_cast<uint32_t*>(h->r + col * 128 + ((gd / 4 ^ col % 8) * 16) + gd % 4 * 4) = __builtin_amdgcn_perm(q, p, 0x05040100u);
-                    *reinterpret_cast<uint32_t*>(h->r + (col + 1) * 128 + ((gd / 4 ^ (col + 1) % 8) * 16) + gd % 4 * 4) =
+                    *reinterpret_cast<uint32_t*>(h->r + col * 128 + ((gd / 4 ^ col / 2 % 8) * 16) + gd % 4 * 4) = __builtin_amdgcn_perm(q, p, 0x05040100u);
+                    *reinterpret_cast<uint32_t*>(h->r + (col + 1) * 128 + ((gd / 4 ^ col / 2 % 8) * 16) + gd % 4 * 4) =
                         __builtin_amdgcn_perm(q, p, 0x07060302u);
                 });
         }
@@ -196,18 +216,18 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
             for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(h->sr + (wj + b * 32 + l32) * 8 + g * 4) & keep;
         }
         if constexpr (OP == LINEAR) {
-            const uint32_t blk = s / A.terms * 2 + g;
+            const uint32_t blk = right_step(s) * 2 + g;
 #pragma unroll
             for (int b = 0; b < TN; b++) {
-                S.w[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + g * 16);
+                S.w[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + (g ^ l32 / 8 % 2) * 16);
                 const uint32_t sb = h->sr[(wj + b * 32 + l32) * 4 + blk % 4];
-                S.sr[b] = blk < nb ? sb << 23 : 0;
+                S.sr[b] = blk < nb ? sb : 0;
             }
         }
     }
 
     __device__ __forceinline__ void load_frag(int j, const Half* __restrict h, Frag& F) {
-        const uint32_t c = ((g * 4 + j) ^ l32 % 8) * 16;
+        const uint32_t c = ((g * 4 + j) ^ l32 / 2 % 8) * 16;
 #pragma unroll
         for (int a = 0; a < TM; a++) F.x[a] = *reinterpret_cast<const i32x4*>(h->l + (wm + a * 32 + l32) * 128 + c);
         if constexpr (OP != LINEAR)
@@ -215,32 +235,57 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
             for (int b = 0; b < TN; b++) F.y[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + c);
     }
 
-    template <int j> __device__ __forceinline__ void multiply(Frag& F, const Side& S, f32x16 (&acc)[TM][TN]) {
+    // linear: the right's part of a fragment, from four bits.
+    template <int j> __device__ __forceinline__ void widen(const Side& S, Frag& F) {
         if constexpr (OP == LINEAR)
 #pragma unroll
             for (int b = 0; b < TN; b++)
                 unroll4([&](auto B) {
-                    F.y[b][B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(S.w[b][j], __int_as_float(S.sr[b]), B.value));
+                    F.y[b][B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(S.w[b][j], mx_scale(S.sr[b]), B.value));
                 });
+    }
+
+    template <int j> __device__ __forceinline__ void multiply(const Frag& F, const Side& S, f32x16 (&acc)[TM][TN]) {
 #pragma unroll
         for (int a = 0; a < TM; a++)
 #pragma unroll
             for (int b = 0; b < TN; b++)
                 if constexpr (OP == PRODUCT) {
                     const i32x8 x = { F.x[a][0], F.x[a][1], F.x[a][2], F.x[a][3], 0, 0, 0, 0 }, y = { F.y[b][0], F.y[b][1], F.y[b][2], F.y[b][3], 0, 0, 0, 0 };
-                    acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc[a][b], 4, 4, j, S.sl[a], j, S.sr[b]);
+                    acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y, x, acc[a][b], 4, 4, j, S.sr[b], j, S.sl[a]);
                 } else {
-                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, F.x[a]), __builtin_bit_cast(bf16x8, F.y[b]), acc[a][b], 0, 0, 0);
+                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, F.y[b]), __builtin_bit_cast(bf16x8, F.x[a]), acc[a][b], 0, 0, 0);
                 }
     }
 
     static __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
-    // This wave's loads have arrived and its reads are done, and so are everyone's.
+    // This wave's loads have arrived, its reads and writes of shared memory are done, and so are everyone's.
     static __device__ __forceinline__ void meet() {
         pin();
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);                            // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        pin();
+    }
+
+    // The order of a quarter of a step: `gap` matrix instructions, then a read of shared memory and `loads` loads, and so on; the rest between.
+    static constexpr int kGap = TM * TN / (TM + (OP == LINEAR ? 0 : TN));
+    template <int gap, int loads, bool turning = false> static __device__ __forceinline__ void order() {
+#pragma unroll
+        for (int i = 0; i < TM * TN / gap; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x8, gap, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (loads) __builtin_amdgcn_sched_group_barrier(0x10, loads ? loads : 1, 0);
+            if (OP == LINEAR) __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+            if (OP == GRAD && turning)
+#pragma unroll
+                for (int k = 0; k < (int)PW / (TM * TN / gap); k++) {
+                    __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                }
+        }
         pin();
     }
 
@@ -249,46 +294,80 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
         Frag F1, F2, F3;
         load_frag(1, cur, F1);
-        pin();
+        widen<1>(S, F1);
+        fetch_rest(s + 1, next);
         multiply<0>(F, S, acc);
-        pin();
+        order<kGap, 2>();
         load_frag(2, cur, F2);
-        pin();
+        widen<2>(S, F2);
         multiply<1>(F1, S, acc);
-        pin();
+        order<kGap, 0>();
         load_frag(3, cur, F3);
-        pin();
-        multiply<2>(F2, S, acc);
+        widen<3>(S, F3);
         turn(next);
+        multiply<2>(F2, S, acc);
+        order<kGap, 0, true>();
         meet();
         fetch(s + 2, cur);
         Side S1;
         load_side(s + 1, next, S1);
         load_frag(0, next, F);
+        widen<0>(S1, F);
         multiply<3>(F3, S, acc);
-#pragma unroll
-        for (int i = 0; i < TM * TN; i++) {                            // one matrix instruction, one read, two loads, and so on
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x10, 2, 0);
-        }
-        pin();
+        order<1, 1>();
         S = S1;
     }
 
-    template <typename T> __device__ __forceinline__ void store(const f32x16 (&acc)[TM][TN]) {
-        T* const c = reinterpret_cast<T*>(A.c) + m0 * A.ldc + j0;
+    // The wave's part of C, 32 rows at a time, through a part of a half's memory: a lane holds 4 neighbouring columns of a row (the right is
+    // the matrix instructions' first operand), and leaves with 16 bytes of a row next to those of its neighbours.
+    template <typename T> __device__ __forceinline__ void store(uint8_t* scratch, const f32x16 (&acc)[TM][TN]) {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        constexpr int B = out_tiles(sizeof(T));
+        static_assert(B >= 1 && TN % B == 0, "");
+        constexpr uint32_t W = B * 32, E = 16 / sizeof(T);             // columns of a pass; elements of 16 bytes
+        constexpr uint32_t P = out_bytes(B, sizeof(T));
+        uint8_t* const mine = scratch + wave * 32 * P;
+        const rsrc_t rc = buffer_at(reinterpret_cast<T*>(A.c) + m0 * A.ldc + j0);
+        const uint32_t pitch = (uint32_t)A.ldc * (uint32_t)sizeof(T);
+        const bool wide = pitch % 16 == 0;
 #pragma unroll
         for (int a = 0; a < TM; a++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const uint32_t m = wm + a * 32 + i / 4 * 8 + g * 4 + i % 4;
+            for (int b0 = 0; b0 < TN; b0 += B) {
 #pragma unroll
-                for (int b = 0; b < TN; b++) {
-                    const uint32_t j = wj + b * 32 + l32;
-                    if (m < rows && j < cols) c[m * A.ldc + j] = (T)acc[a][b][i];
+                for (int b = 0; b < B; b++)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const f32x16& c = acc[a][b0 + b];
+                        const t4 v = { (T)c[i], (T)c[i + 1], (T)c[i + 2], (T)c[i + 3] };
+                        *reinterpret_cast<t4*>(mine + l32 * P + (b * 32 + i * 2 + g * 4) * sizeof(T)) = v;
+                    }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                const uint32_t m1 = wm + a * 32, j1 = wj + b0 * 32;
+                if (wide) {
+#pragma unroll
+                    for (uint32_t r = 0; r < 32; r += 64 * E / W) {
+                        const uint32_t row = r + lane / (W / E), col = lane % (W / E) * E, m = m1 + row, j = j1 + col;
+                        const i32x4 v = *reinterpret_cast<const i32x4*>(mine + row * P + col * sizeof(T));
+                        const uint32_t off = m * pitch + j * (uint32_t)sizeof(T);
+                        __builtin_amdgcn_raw_buffer_store_b128(v, rc, m < rows && j + E <= cols ? off : kNowhere, 0, 0);
+                        if (m < rows && j < cols && j + E > cols)
+                            for (uint32_t e = 0; j + e < cols; e++)
+                                put(rc, reinterpret_cast<const T*>(mine + row * P)[col + e], off + e * (uint32_t)sizeof(T));
+                    }
+                } else {
+                    for (uint32_t e = lane; e < 32 * W; e += 64) {
+                        const uint32_t row = e / W, col = e % W, m = m1 + row, j = j1 + col;
+                        put(rc, reinterpret_cast<const T*>(mine + row * P)[col], m < rows && j < cols ? m * pitch + j * (uint32_t)sizeof(T) : kNowhere);
+                    }
                 }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
+    }
+
+    template <typename T> static __device__ __forceinline__ void put(rsrc_t r, T v, uint32_t off) {
+        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, off, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), r, off, 0, 0);
     }
 };
 
@@ -303,6 +382,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
 #pragma unroll
         for (int b = 0; b < Tl::TN; b++) acc[a][b] = f32x16{};
     T.fetch(0, &h0);
+    T.fetch_rest(0, &h0);
     T.turn(&h0);
     T.fetch(1, &h1);
     T.meet();
@@ -310,16 +390,18 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     typename Tl::Side S;
     T.load_side(0, &h0, S);
     T.load_frag(0, &h0, F);
+    T.template widen<0>(S, F);
     uint32_t s = 0;
     for (; s + 1 < A.steps; s += 2) {
         T.step(s, &h0, &h1, F, S, acc);
         T.step(s + 1, &h1, &h0, F, S, acc);
     }
     if (s < A.steps) T.step(s, &h0, &h1, F, S, acc);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                   // no load may reach shared memory after the workgroup's end
-    if (A.c_type == F32) T.template store<float>(acc);
-    else if (A.c_type == BF16) T.template store<__bf16>(acc);
-    else T.template store<_Float16>(acc);
+    Tl::meet();                                                        // (nor may a load reach shared memory after the workgroup's end)
+    uint8_t* const scratch = reinterpret_cast<uint8_t*>(&h0);
+    if (A.c_type == F32) T.template store<float>(scratch, acc);
+    else if (A.c_type == BF16) T.template store<__bf16>(scratch, acc);
+    else T.template store<_Float16>(scratch, acc);
 }
 
 // Floats of the left as bf16 terms that add up to them: one for bf16, two for fp16 (11 bits), three for float32 (24 bits).  Each term
@@ -406,6 +488,7 @@ hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStre
         T.left = reinterpret_cast<const uint8_t*>(ws); T.left_pitch = (uint64_t)chunks * 128 * T.terms;
     }
     T.steps = chunks * T.terms;
+    T.per_term = (0x80000000u + T.terms - 1) / T.terms;
     return kind == LINEAR ? launch_tiles<LINEAR>(T, st) : launch_tiles<GRAD>(T, st);
 }
 
