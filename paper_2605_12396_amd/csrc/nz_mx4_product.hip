@@ -13,6 +13,7 @@ enum : int { PRODUCT = 0, LINEAR = 1, GRAD = 2 };
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
@@ -404,38 +405,259 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     else T.template store<_Float16>(scratch, acc);
 }
 
-// Floats of the left as bf16 terms that add up to them: one for bf16, two for fp16 (11 bits), three for float32 (24 bits).  Each term
-// takes the top of what is left, cut off (not rounded, which could carry past the largest float32), so every difference is exact; an
-// infinity or NaN is its first term alone.  Rows become whole steps of 64 elements, term after term in a step, zeros behind the end.
+// A float as bf16 terms that add up to it: one for bf16, two for fp16 (11 bits), three for float32 (24 bits).  Each term takes the top of
+// what is left, cut off (not rounded, which could carry past the largest float32), so every difference is exact; an infinity or NaN is its
+// first term alone.  top: the terms' bits in the upper half of a word.
+__host__ __device__ constexpr int terms_of(int type) { return type == F32 ? 3 : type == F16 ? 2 : 1; }
+
+template <int T> __device__ __forceinline__ void cut(float v, uint32_t (&top)[terms_of(T)]) {
+    const bool plain = (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
+#pragma unroll
+    for (int q = 0; q < terms_of(T); q++) {
+        top[q] = __float_as_uint(v) & 0xFFFF0000u;
+        if (q == 0 && v != v) top[q] |= 0x00400000u;
+        if (q > 0 && !plain) top[q] = 0;
+        v -= __uint_as_float(top[q]);
+    }
+}
+
+// Eight floats as they lie in memory: loaded in 16-byte words, or one by one with zeros for those past the end; then cut into terms.
+template <int T> struct Eight {
+    i32x4 w[float_bytes(T) / 2];
+
+    // off: of the first in bytes, or kNowhere
+    __device__ __forceinline__ void load_words(rsrc_t r, uint32_t off) {
+#pragma unroll
+        for (uint32_t i = 0; i < float_bytes(T) / 2; i++) w[i] = load16(r, off == kNowhere ? off : off + i * 16);
+    }
+
+    __device__ __forceinline__ void load_each(rsrc_t r, uint32_t off, uint32_t n) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) {
+            const uint32_t at = i < n ? off + i * float_bytes(T) : kNowhere;
+            if (T == F32) w[i / 4][i % 4] = __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+            else {
+                const uint32_t v = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+                w[0][i / 2] = i % 2 ? (int)((uint32_t)w[0][i / 2] | v << 16) : (int)v;
+            }
+        }
+    }
+
+    __device__ __forceinline__ float value(int i) const {
+        if (T == F32) return __int_as_float(w[i / 4][i % 4]);
+        const uint16_t h = (uint16_t)((uint32_t)w[0][i / 2] >> (i % 2 * 16));
+        return T == F16 ? (float)__builtin_bit_cast(_Float16, h) : __uint_as_float((uint32_t)h << 16);
+    }
+
+    __device__ __forceinline__ void terms(i32x4 (&out)[terms_of(T)]) const {
+        if constexpr (T == BF16) { out[0] = w[0]; return; }
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint32_t a[terms_of(T)], b[terms_of(T)];
+            cut<T>(value(2 * i), a);
+            cut<T>(value(2 * i + 1), b);
+#pragma unroll
+            for (int q = 0; q < terms_of(T); q++) out[q][i] = (int)(a[q] >> 16 | b[q]);
+        }
+    }
+};
+
+// The left for the tiles: rows of whole steps of 64 elements, term after term in a step, zeros behind the end.
 template <int T>
-__global__ __launch_bounds__(256) void k_mx_terms(const void* x, uint64_t ldx, uint64_t M, uint64_t inner, uint32_t chunks, uint16_t* out) {
-    constexpr int terms = T == F32 ? 3 : T == F16 ? 2 : 1;
+__global__ __launch_bounds__(256) void k_mx_terms(const uint8_t* x, uint64_t ldx, bool wide, uint64_t M, uint64_t inner, uint32_t chunks,
+                                                  uint16_t* out) {
+    constexpr int terms = terms_of(T);
     const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;               // 8 elements
     const uint64_t per_row = (uint64_t)chunks * 8;
     const uint64_t m = id / per_row;
     if (m >= M) return;
     const uint64_t o = id % per_row, i0 = o * 8;
-    uint32_t w[terms][4];
-    for (int i = 0; i < 8; i++) {
-        float v = 0.0f;
-        if (i0 + i < inner) {
-            const uint64_t at = m * ldx + i0 + i;
-            if (T == F32) v = reinterpret_cast<const float*>(x)[at];
-            else if (T == F16) v = (float)reinterpret_cast<const _Float16*>(x)[at];
-            else v = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(x)[at] << 16);
-        }
-        const bool plain = (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
-        for (int q = 0; q < terms; q++) {
-            uint32_t top = __float_as_uint(v) & 0xFFFF0000u;
-            if (q == 0 && v != v) top |= 0x00400000u;
-            if (q > 0 && !plain) top = 0;
-            v -= __uint_as_float(top);
-            if (i % 2 == 0) w[q][i / 2] = top >> 16; else w[q][i / 2] |= top;
-        }
-    }
+    const uint32_t n = i0 >= inner ? 0 : (uint32_t)min(inner - i0, (uint64_t)8);
+    i32x4 w[terms];
+    Eight<T> e;
+    const rsrc_t r = buffer_at(x + m * ldx * float_bytes(T));
+    if (wide && n == 8) e.load_words(r, (uint32_t)i0 * float_bytes(T)); else e.load_each(r, (uint32_t)i0 * float_bytes(T), n);
+    e.terms(w);
     uint16_t* const at = out + m * chunks * 64 * terms + (o / 8) * 64 * terms + o % 8 * 8;
-    for (int q = 0; q < terms; q++) *reinterpret_cast<uint4*>(at + q * 64) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    for (int q = 0; q < terms; q++) *reinterpret_cast<i32x4*>(at + q * 64) = w[q];
 }
+
+// The left for k_mx_rows: a thread copies 16 bytes, zeros behind the end of a row.
+template <int SIZE>
+__global__ __launch_bounds__(256) void k_mx_lay(const uint8_t* x, uint64_t pitch, uint32_t M, uint64_t inner, uint8_t* out) {
+    constexpr uint32_t E = 16 / SIZE;
+    const uint64_t per_row = (inner + 7) / 8 * 8 / E, id = (uint64_t)blockIdx.x * 256 + threadIdx.x, m = id / per_row, i0 = id % per_row * E;
+    if (m >= M) return;
+    i32x4 w = {};
+#pragma unroll
+    for (uint32_t i = 0; i < E; i++)
+        if (i0 + i < inner) {
+            if (SIZE == 4) w[i % 4] = reinterpret_cast<const int*>(x + m * pitch)[i0 + i];
+            else w[i / 2 % 4] |= (int)((uint32_t)reinterpret_cast<const uint16_t*>(x + m * pitch)[i0 + i] << (i % 2 * 16));
+        }
+    reinterpret_cast<i32x4*>(out)[id] = w;
+}
+
+struct RowArgs {
+    const uint8_t* left; uint64_t left_pitch;             // codes or floats, and bytes of a row
+    const uint8_t* left_scales; uint64_t left_spitch;
+    const uint8_t* right; uint64_t right_pitch; const uint8_t* right_scales; uint64_t right_spitch;
+    uint32_t M; uint64_t outer, inner;
+    void* c; uint64_t ldc; int c_type;
+};
+
+__device__ __forceinline__ void store_one(void* c, int type, uint64_t at, float v) {
+    if (type == F32) reinterpret_cast<float*>(c)[at] = v;
+    else if (type == BF16) reinterpret_cast<__bf16*>(c)[at] = (__bf16)v;
+    else reinterpret_cast<_Float16*>(c)[at] = (_Float16)v;
+}
+
+// Few rows on the left: bound by the codes of the right, which pass once from memory through registers to the matrix units.
+// A workgroup of 8 waves makes 16 NJ columns of up to 16 MF rows; each wave sums over an eighth of the length, and the eighths are added in
+// their order at the end.  A wave takes S units of 128 elements at a time: it asks for all of the right's codes of these units, then for
+// the left's, which serve all NJ tiles of 16 columns.  LEFT: type of the floats (then a unit is four matrix instructions a term, lane group
+// g = lane / 16 taking elements 32 g + 8 j .. + 7 in the j-th), or -1 for four bits (one instruction, group g taking block g).
+template <int LEFT, int MF, int NJ>
+__global__ __launch_bounds__(512, 1) void k_mx_rows(RowArgs A) {
+    constexpr int T = LEFT < 0 ? BF16 : LEFT;
+    constexpr int terms = terms_of(T);
+    constexpr int S = LEFT < 0 ? (MF == 4 ? 4 : 8) : MF * terms >= 8 ? 1 : MF * terms >= 3 ? 2 : MF * terms == 2 ? 4 : 8;
+    constexpr int XN = LEFT < 0 ? 1 : 4 * terms;                        // fragments of a unit and 16 rows
+    __shared__ float part[8][MF * NJ][256];
+    const uint32_t t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), r16 = lane % 16, g = lane / 16;
+    const uint64_t j0 = (uint64_t)blockIdx.x * (16 * NJ);
+    const uint32_t cols = (uint32_t)min(A.outer - j0, (uint64_t)(16 * NJ));
+    const uint32_t nb = (uint32_t)((A.inner + 31) / 32), units = (nb + 3) / 4;
+    const uint32_t u0 = (uint32_t)((uint64_t)units * wave / 8), u1 = (uint32_t)((uint64_t)units * (wave + 1) / 8);
+
+    f32x4 acc[MF][NJ];
+#pragma unroll
+    for (int a = 0; a < MF; a++)
+#pragma unroll
+        for (int b = 0; b < NJ; b++) acc[a][b] = f32x4{};
+    uint32_t ro[NJ], so[NJ], lo[MF], lso[MF];
+#pragma unroll
+    for (int b = 0; b < NJ; b++) {
+        const uint32_t j = min(b * 16 + r16, cols - 1);
+        ro[b] = j * (uint32_t)A.right_pitch + g * 16;
+        so[b] = j * (uint32_t)A.right_spitch;
+    }
+#pragma unroll
+    for (int a = 0; a < MF; a++) {
+        const uint32_t m = min(a * 16 + r16, A.M - 1);
+        lo[a] = m * (uint32_t)A.left_pitch + (LEFT < 0 ? g * 16 : 0);
+        lso[a] = m * (uint32_t)A.left_spitch;
+    }
+
+    for (uint32_t u = u0; u < u1; u += S) {
+        const rsrc_t br = buffer_at(A.right + j0 * A.right_pitch + (uint64_t)u * 64), bs = buffer_at(A.right_scales + j0 * A.right_spitch + (uint64_t)u * 4);
+        i32x4 w[S][NJ];
+        uint32_t sc[S][NJ];
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int b = 0; b < NJ; b++) {
+                const bool in = (u + s < u1) & ((u + s) * 4 + g < nb);
+                w[s][b] = load16(br, in ? ro[b] + s * 64 : kNowhere);
+                sc[s][b] = __builtin_amdgcn_raw_buffer_load_b32(bs, in ? so[b] + s * 4 : kNowhere, 0, 0);
+            }
+        i32x4 x[S][MF][XN];
+        uint32_t xs[S][MF];
+        if constexpr (LEFT < 0) {
+            const rsrc_t bl = buffer_at(A.left + (uint64_t)u * 64), bls = buffer_at(A.left_scales + (uint64_t)u * 4);
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int a = 0; a < MF; a++) {
+                    const bool in = (u + s < u1) & ((u + s) * 4 + g < nb);
+                    x[s][a][0] = load16(bl, in ? lo[a] + s * 64 : kNowhere);
+                    xs[s][a] = __builtin_amdgcn_raw_buffer_load_b32(bls, in ? lso[a] + s * 4 : kNowhere, 0, 0);
+                }
+        } else {
+            const rsrc_t bl = buffer_at(A.left + (uint64_t)u * 128 * float_bytes(T));
+            Eight<T> e[S][MF][4];
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int a = 0; a < MF; a++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const uint32_t i = s * 128 + g * 32 + j * 8;
+                        const bool in = (u + s < u1) & ((uint64_t)u * 128 + i < A.inner);
+                        e[s][a][j].load_words(bl, in ? lo[a] + i * float_bytes(T) : kNowhere);
+                    }
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int a = 0; a < MF; a++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        i32x4 v[terms];
+                        e[s][a][j].terms(v);
+#pragma unroll
+                        for (int q = 0; q < terms; q++) x[s][a][j * terms + q] = v[q];
+                    }
+        }
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int b = 0; b < NJ; b++) {
+                const uint32_t sb = __builtin_amdgcn_ubfe(sc[s][b], 8 * g, 8);
+                if constexpr (LEFT < 0) {
+#pragma unroll
+                    for (int a = 0; a < MF; a++) {
+                        const uint32_t sa = __builtin_amdgcn_ubfe(xs[s][a], 8 * g, 8);
+                        const i32x4 p = x[s][a][0], q = w[s][b];
+                        const i32x8 p8 = { p[0], p[1], p[2], p[3], 0, 0, 0, 0 }, q8 = { q[0], q[1], q[2], q[3], 0, 0, 0, 0 };
+                        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p8, q8, acc[a][b], 4, 4, 0, sa, 0, sb);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        i32x4 y;
+                        unroll4([&](auto B) { y[B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[s][b][j], mx_scale(sb), B.value)); });
+#pragma unroll
+                        for (int a = 0; a < MF; a++)
+#pragma unroll
+                            for (int q = 0; q < terms; q++)
+                                acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[s][a][j * terms + q]),
+                                                                                    __builtin_bit_cast(bf16x8, y), acc[a][b], 0, 0, 0);
+                    }
+                }
+            }
+    }
+
+#pragma unroll
+    for (int a = 0; a < MF; a++)
+#pragma unroll
+        for (int b = 0; b < NJ; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) part[wave][a * NJ + b][(g * 4 + i) * 16 + r16] = acc[a][b][i];
+    __syncthreads();
+    for (uint32_t e = t; e < MF * 16 * NJ * 16; e += 512) {
+        const uint32_t m = e / (16 * NJ), j = e % (16 * NJ);
+        if (m >= A.M || j >= cols) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; k++) v += part[k][m / 16 * NJ + j / 16][m % 16 * 16 + j % 16];
+        store_one(A.c, A.c_type, m * A.ldc + j0 + j, v);
+    }
+}
+
+template <int LEFT, int MF> void launch_rows(const RowArgs& R, hipStream_t st) {
+    const uint64_t tiles = (R.outer + 15) / 16;
+    if (tiles >= 512) hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 2>), dim3((uint32_t)((tiles + 1) / 2)), dim3(512), 0, st, R);
+    else hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 1>), dim3((uint32_t)tiles), dim3(512), 0, st, R);
+}
+
+template <int LEFT> hipError_t launch_rows(const RowArgs& R, hipStream_t st) {
+    if (R.M <= 16) launch_rows<LEFT, 1>(R, st);
+    else if (R.M <= 32) launch_rows<LEFT, 2>(R, st);
+    else launch_rows<LEFT, 4>(R, st);
+    return hipGetLastError();
+}
+
+constexpr uint64_t kFewRows = 64;
 
 template <int OP, int BM, int BN, int WM, int WN> void launch_tile(const TileArgs& T, hipStream_t st) {
     hipLaunchKernelGGL((k_mx_tile<OP, BM, BN, WM, WN>), dim3(T.tiles_m * T.tiles_j), dim3(64 * WM * WN), 0, st, T);
@@ -454,15 +676,44 @@ template <int OP> hipError_t launch_tiles(TileArgs& T, hipStream_t st) {
 // Whether the matrix instructions can be fed from the caller's rows: bf16, rows and their ends at multiples of 16 bytes.
 bool fed_directly(const MxProductArgs& A, uint64_t inner, int left) { return left == BF16 && A.ldx % 8 == 0 && inner % 8 == 0; }
 
+template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint32_t chunks, hipStream_t st) {
+    hipLaunchKernelGGL((k_mx_terms<T>), dim3((uint32_t)((A.M * chunks * 8 + 255) / 256)), dim3(256), 0, st, reinterpret_cast<const uint8_t*>(A.x), A.ldx,
+                       A.ldx * float_bytes(T) % 16 == 0, A.M, inner, chunks, reinterpret_cast<uint16_t*>(A.ws));
+}
+
 }  // namespace
 
 size_t mx_product_workspace(int kind, int left, uint64_t M, uint64_t N, uint64_t K) {
     if (kind == PRODUCT) return 0;
+    if (kind == LINEAR && M <= kFewRows) return M * ((K + 7) / 8 * 8) * float_bytes(left);
     const uint64_t inner = kind == GRAD ? N : K;
-    return (inner + 63) / 64 * 128 * M * (left == F32 ? 3 : left == F16 ? 2 : 1);
+    return (inner + 63) / 64 * 128 * M * terms_of(left);
 }
 
 hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStream_t st) {
+    if (kind != GRAD && A.M <= kFewRows) {
+        RowArgs R = {};
+        R.right = A.b.codes; R.right_pitch = A.b.pitch * 16; R.right_scales = A.b.scales; R.right_spitch = A.b.pitch;
+        R.M = (uint32_t)A.M; R.outer = A.N; R.inner = A.K;
+        R.c = A.c; R.ldc = A.ldc; R.c_type = A.c_type;
+        if (kind == PRODUCT) {
+            R.left = A.a.codes; R.left_pitch = A.a.pitch * 16; R.left_scales = A.a.scales; R.left_spitch = A.a.pitch;
+            return launch_rows<-1>(R, st);
+        }
+        R.left = reinterpret_cast<const uint8_t*>(A.x); R.left_pitch = A.ldx * float_bytes(left);
+        if ((A.M > 1 && R.left_pitch % 16) || A.K % 8) {
+            const uint64_t row = (A.K + 7) / 8 * 8 * float_bytes(left);
+            uint8_t* const ws = reinterpret_cast<uint8_t*>(A.ws);
+            const dim3 grid((uint32_t)((A.M * row / 16 + 255) / 256));
+            if (left == F32) hipLaunchKernelGGL((k_mx_lay<4>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
+            else hipLaunchKernelGGL((k_mx_lay<2>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            R.left = ws; R.left_pitch = row;
+            R.inner = (A.K + 7) / 8 * 8;                          // (the codes there are 0)
+        }
+        return left == F32 ? launch_rows<F32>(R, st) : left == F16 ? launch_rows<F16>(R, st) : launch_rows<BF16>(R, st);
+    }
     TileArgs T = {};
     T.M = A.M; T.outer = kind == GRAD ? A.K : A.N; T.inner = kind == GRAD ? A.N : A.K;
     T.c = A.c; T.ldc = A.ldc; T.c_type = A.c_type;
@@ -477,15 +728,13 @@ hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStre
     if (fed_directly(A, T.inner, left)) {
         T.left = reinterpret_cast<const uint8_t*>(A.x); T.left_pitch = A.ldx * 2;
     } else {
-        T.terms = left == F32 ? 3 : left == F16 ? 2 : 1;
-        const uint32_t grid = (uint32_t)((A.M * chunks * 8 + 255) / 256);
-        uint16_t* const ws = reinterpret_cast<uint16_t*>(A.ws);
-        if (left == F32) hipLaunchKernelGGL((k_mx_terms<F32>), dim3(grid), dim3(256), 0, st, A.x, A.ldx, A.M, T.inner, chunks, ws);
-        else if (left == F16) hipLaunchKernelGGL((k_mx_terms<F16>), dim3(grid), dim3(256), 0, st, A.x, A.ldx, A.M, T.inner, chunks, ws);
-        else hipLaunchKernelGGL((k_mx_terms<BF16>), dim3(grid), dim3(256), 0, st, A.x, A.ldx, A.M, T.inner, chunks, ws);
+        T.terms = terms_of(left);
+        if (left == F32) launch_terms<F32>(A, T.inner, chunks, st);
+        else if (left == F16) launch_terms<F16>(A, T.inner, chunks, st);
+        else launch_terms<BF16>(A, T.inner, chunks, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        T.left = reinterpret_cast<const uint8_t*>(ws); T.left_pitch = (uint64_t)chunks * 128 * T.terms;
+        T.left = reinterpret_cast<const uint8_t*>(A.ws); T.left_pitch = (uint64_t)chunks * 128 * T.terms;
     }
     T.steps = chunks * T.terms;
     T.per_term = (0x80000000u + T.terms - 1) / T.terms;
