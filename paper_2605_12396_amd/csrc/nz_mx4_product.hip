@@ -514,34 +514,38 @@ __device__ __forceinline__ void store_one(void* c, int type, uint64_t at, float 
 
 // Few rows on the left: bound by the codes of the right, which pass once from memory through registers to the matrix units.
 // A workgroup of 8 waves makes 16 NJ columns of up to 16 MF rows; each wave sums over an eighth of the length, and the eighths are added in
-// their order at the end.  A wave takes S units of 128 elements at a time: it asks for all of the right's codes of these units, then for
-// the left's, which serve all NJ tiles of 16 columns.  LEFT: type of the floats (then a unit is four matrix instructions a term, lane group
-// g = lane / 16 taking elements 32 g + 8 j .. + 7 in the j-th), or -1 for four bits (one instruction, group g taking block g).
-template <int LEFT, int MF, int NJ>
-__global__ __launch_bounds__(512, 1) void k_mx_rows(RowArgs A) {
+// their order at the end.  A wave takes S units of 128 elements at a time: it asks for all of the right's codes of these units, for their
+// scales, which it spreads through shared memory of its own (a load for every unit would read four bytes of a row at a time), and for the
+// left, which serves all NJ tiles of 16 columns.  LEFT: type of the floats (then a unit is four matrix instructions a term, lane group
+// g = lane / 16 taking elements 32 g + 8 j .. + 7 in the j-th; rows start at multiples of 16 bytes and have a multiple of 8 elements), or -1
+// for four bits (one instruction, group g taking block g).
+// The matrix instructions take 16 rows whether there are as many or not.  FEW: up to 4 rows, which also come through shared memory, each
+// byte loaded once; else every lane loads the fragments that it multiplies.
+template <int LEFT, int MF, int NJ, bool FEW>
+__global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
     constexpr int T = LEFT < 0 ? BF16 : LEFT;
     constexpr int terms = terms_of(T);
-    constexpr int S = LEFT < 0 ? (MF == 4 ? 4 : 8) : MF * terms >= 8 ? 1 : MF * terms >= 3 ? 2 : MF * terms == 2 ? 4 : 8;
-    constexpr int XN = LEFT < 0 ? 1 : 4 * terms;                        // fragments of a unit and 16 rows
-    __shared__ float part[8][MF * NJ][256];
+    constexpr int S = LEFT < 0 ? (MF == 4 ? 4 : 8) : FEW ? (T == F32 ? 4 : 8) : MF * terms >= 8 ? 1 : MF * terms >= 3 ? 2 : MF * terms == 2 ? 4 : 8;
+    constexpr uint32_t LB = LEFT < 0 ? S * 64 : S * 128 * float_bytes(T);                     // bytes of a row of the left and S units
+    constexpr uint32_t kScaleWords = 16 * NJ * S, kLeftBytes = FEW ? 4 * LB : 0, kLeftScales = FEW && LEFT < 0 ? 4 * S * 4 : 0;
+    struct Own { uint8_t left[kLeftBytes + 16]; uint32_t scales[kScaleWords]; uint32_t left_scales[kLeftScales / 4 + 4]; };
+    union Shared { Own own[8]; float part[8][MF * NJ][256]; };
+    __shared__ __attribute__((aligned(16))) Shared sh;
     const uint32_t t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), r16 = lane % 16, g = lane / 16;
     const uint64_t j0 = (uint64_t)blockIdx.x * (16 * NJ);
     const uint32_t cols = (uint32_t)min(A.outer - j0, (uint64_t)(16 * NJ));
     const uint32_t nb = (uint32_t)((A.inner + 31) / 32), units = (nb + 3) / 4;
     const uint32_t u0 = (uint32_t)((uint64_t)units * wave / 8), u1 = (uint32_t)((uint64_t)units * (wave + 1) / 8);
+    Own& own = sh.own[wave];
 
     f32x4 acc[MF][NJ];
 #pragma unroll
     for (int a = 0; a < MF; a++)
 #pragma unroll
         for (int b = 0; b < NJ; b++) acc[a][b] = f32x4{};
-    uint32_t ro[NJ], so[NJ], lo[MF], lso[MF];
+    uint32_t ro[NJ], lo[MF], lso[MF];
 #pragma unroll
-    for (int b = 0; b < NJ; b++) {
-        const uint32_t j = min(b * 16 + r16, cols - 1);
-        ro[b] = j * (uint32_t)A.right_pitch + g * 16;
-        so[b] = j * (uint32_t)A.right_spitch;
-    }
+    for (int b = 0; b < NJ; b++) ro[b] = min(b * 16 + r16, cols - 1) * (uint32_t)A.right_pitch + g * 16;
 #pragma unroll
     for (int a = 0; a < MF; a++) {
         const uint32_t m = min(a * 16 + r16, A.M - 1);
@@ -551,109 +555,152 @@ __global__ __launch_bounds__(512, 1) void k_mx_rows(RowArgs A) {
 
     for (uint32_t u = u0; u < u1; u += S) {
         const rsrc_t br = buffer_at(A.right + j0 * A.right_pitch + (uint64_t)u * 64), bs = buffer_at(A.right_scales + j0 * A.right_spitch + (uint64_t)u * 4);
+        const rsrc_t bl = buffer_at(A.left + (uint64_t)u * LB / S), bls = buffer_at(A.left_scales + (uint64_t)u * 4);
+        // the right's codes
         i32x4 w[S][NJ];
-        uint32_t sc[S][NJ];
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int b = 0; b < NJ; b++) {
-                const bool in = (u + s < u1) & ((u + s) * 4 + g < nb);
-                w[s][b] = load16(br, in ? ro[b] + s * 64 : kNowhere);
-                sc[s][b] = __builtin_amdgcn_raw_buffer_load_b32(bs, in ? so[b] + s * 4 : kNowhere, 0, 0);
-            }
-        i32x4 x[S][MF][XN];
+            for (int b = 0; b < NJ; b++) w[s][b] = load16(br, (u + s < u1) & ((u + s) * 4 + g < nb) ? ro[b] + s * 64 : kNowhere);
+        // its scales, a word a unit
+        constexpr uint32_t SW = (kScaleWords + 63) / 64;
+        uint32_t sw[SW];
+#pragma unroll
+        for (uint32_t i = 0; i < SW; i++) {
+            const uint32_t e = i * 64 + lane, row = e / S, un = e % S;
+            sw[i] = __builtin_amdgcn_raw_buffer_load_b32(bs, u + un < u1 ? min(row, cols - 1) * (uint32_t)A.right_spitch + un * 4 : kNowhere, 0, 0);
+        }
+        // the left
+        i32x4 x[FEW ? 1 : S][MF][FEW ? 1 : LEFT < 0 ? 1 : 4 * terms];
         uint32_t xs[S][MF];
-        if constexpr (LEFT < 0) {
-            const rsrc_t bl = buffer_at(A.left + (uint64_t)u * 64), bls = buffer_at(A.left_scales + (uint64_t)u * 4);
+        if constexpr (FEW) {
+            constexpr uint32_t LN = kLeftBytes / 1024;                  // (a load of the wave is part of one row or covers whole ones)
+            i32x4 lv[LN];
+            uint32_t ls = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < LN; i++) {
+                const uint32_t e = (i * 64 + lane) * 16, row = e / LB, at = e % LB;
+                const uint64_t end = LEFT < 0 ? (uint64_t)nb * 16 : A.inner * float_bytes(T);           // bytes of a row
+                const bool in = (row < A.M) & (u + at / (LB / S) < u1) & ((uint64_t)u * (LB / S) + at < end);
+                lv[i] = load16(bl, in ? row * (uint32_t)A.left_pitch + at : kNowhere);
+            }
+            if constexpr (LEFT < 0) {
+                const uint32_t row = lane / S, un = lane % S;
+                ls = __builtin_amdgcn_raw_buffer_load_b32(bls, (row < min(A.M, 4u)) & (u + un < u1) ? row * (uint32_t)A.left_spitch + un * 4 : kNowhere, 0, 0);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < SW; i++) if (kScaleWords % 64 == 0 || i * 64 + lane < kScaleWords) own.scales[i * 64 + lane] = sw[i];
+#pragma unroll
+            for (uint32_t i = 0; i < LN; i++) *reinterpret_cast<i32x4*>(&own.left[(i * 64 + lane) * 16]) = lv[i];
+            if (LEFT < 0 && lane < 4 * S) own.left_scales[lane] = ls;
+        } else {
 #pragma unroll
             for (int s = 0; s < S; s++)
 #pragma unroll
                 for (int a = 0; a < MF; a++) {
-                    const bool in = (u + s < u1) & ((u + s) * 4 + g < nb);
-                    x[s][a][0] = load16(bl, in ? lo[a] + s * 64 : kNowhere);
-                    xs[s][a] = __builtin_amdgcn_raw_buffer_load_b32(bls, in ? lso[a] + s * 4 : kNowhere, 0, 0);
+                    if constexpr (LEFT < 0) {
+                        const bool in = (u + s < u1) & ((u + s) * 4 + g < nb);
+                        x[s][a][0] = load16(bl, in ? lo[a] + s * 64 : kNowhere);
+                        xs[s][a] = __builtin_amdgcn_raw_buffer_load_b32(bls, in ? lso[a] + s * 4 : kNowhere, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const uint32_t i = s * 128 + g * 32 + j * 8;
+                            const bool in = (u + s < u1) & ((uint64_t)u * 128 + i < A.inner);
+                            Eight<T> e;
+                            e.load_words(bl, in ? lo[a] + i * float_bytes(T) : kNowhere);
+                            i32x4 v[terms];
+                            e.terms(v);
+#pragma unroll
+                            for (int q = 0; q < terms; q++) x[s][a][j * terms + q] = v[q];
+                        }
+                    }
                 }
-        } else {
-            const rsrc_t bl = buffer_at(A.left + (uint64_t)u * 128 * float_bytes(T));
-            Eight<T> e[S][MF][4];
 #pragma unroll
-            for (int s = 0; s < S; s++)
-#pragma unroll
-                for (int a = 0; a < MF; a++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const uint32_t i = s * 128 + g * 32 + j * 8;
-                        const bool in = (u + s < u1) & ((uint64_t)u * 128 + i < A.inner);
-                        e[s][a][j].load_words(bl, in ? lo[a] + i * float_bytes(T) : kNowhere);
-                    }
-#pragma unroll
-            for (int s = 0; s < S; s++)
-#pragma unroll
-                for (int a = 0; a < MF; a++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        i32x4 v[terms];
-                        e[s][a][j].terms(v);
-#pragma unroll
-                        for (int q = 0; q < terms; q++) x[s][a][j * terms + q] = v[q];
-                    }
+            for (uint32_t i = 0; i < SW; i++) if (kScaleWords % 64 == 0 || i * 64 + lane < kScaleWords) own.scales[i * 64 + lane] = sw[i];
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+
+        const uint32_t few = FEW ? min(r16, A.M - 1) : 0;               // this lane's row of the left
 #pragma unroll
-        for (int s = 0; s < S; s++)
+        for (int s = 0; s < S; s++) {
+            uint32_t sb[NJ];
 #pragma unroll
             for (int b = 0; b < NJ; b++) {
-                const uint32_t sb = __builtin_amdgcn_ubfe(sc[s][b], 8 * g, 8);
-                if constexpr (LEFT < 0) {
+                const uint32_t v = reinterpret_cast<const uint8_t*>(own.scales)[((b * 16 + r16) * S + s) * 4 + g];
+                sb[b] = (u + s) * 4 + g < nb ? v : 0;                   // (a word holds more blocks than the last unit has)
+            }
+            if constexpr (LEFT < 0) {
 #pragma unroll
-                    for (int a = 0; a < MF; a++) {
-                        const uint32_t sa = __builtin_amdgcn_ubfe(xs[s][a], 8 * g, 8);
-                        const i32x4 p = x[s][a][0], q = w[s][b];
+                for (int a = 0; a < MF; a++) {
+                    const uint32_t v = FEW ? (uint32_t)reinterpret_cast<const uint8_t*>(own.left_scales)[(few * S + s) * 4 + g] : __builtin_amdgcn_ubfe(xs[s][a], 8 * g, 8);
+                    const uint32_t sa = (u + s) * 4 + g < nb ? v : 0;
+                    const i32x4 p = FEW ? *reinterpret_cast<const i32x4*>(&own.left[few * LB + s * 64 + g * 16]) : x[FEW ? 0 : s][a][0];
+#pragma unroll
+                    for (int b = 0; b < NJ; b++) {
+                        const i32x4 q = w[s][b];
                         const i32x8 p8 = { p[0], p[1], p[2], p[3], 0, 0, 0, 0 }, q8 = { q[0], q[1], q[2], q[3], 0, 0, 0, 0 };
-                        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p8, q8, acc[a][b], 4, 4, 0, sa, 0, sb);
+                        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p8, q8, acc[a][b], 4, 4, 0, sa, 0, sb[b]);
                     }
-                } else {
+                }
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
+                for (int j = 0; j < 4; j++) {
+                    i32x4 v[terms];
+                    if constexpr (FEW) {
+                        Eight<T> e;
+#pragma unroll
+                        for (uint32_t i = 0; i < float_bytes(T) / 2; i++)
+                            e.w[i] = *reinterpret_cast<const i32x4*>(&own.left[few * LB + (s * 128 + g * 32 + j * 8) * float_bytes(T) + i * 16]);
+                        e.terms(v);
+                    }
+#pragma unroll
+                    for (int b = 0; b < NJ; b++) {
                         i32x4 y;
-                        unroll4([&](auto B) { y[B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[s][b][j], mx_scale(sb), B.value)); });
+                        unroll4([&](auto B) { y[B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[s][b][j], mx_scale(sb[b]), B.value)); });
 #pragma unroll
                         for (int a = 0; a < MF; a++)
 #pragma unroll
                             for (int q = 0; q < terms; q++)
-                                acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[s][a][j * terms + q]),
+                                acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, FEW ? v[q] : x[FEW ? 0 : s][a][FEW ? 0 : j * terms + q]),
                                                                                     __builtin_bit_cast(bf16x8, y), acc[a][b], 0, 0, 0);
                     }
                 }
             }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
+    __syncthreads();                                                    // (the sums take the place of what the waves kept)
 #pragma unroll
     for (int a = 0; a < MF; a++)
 #pragma unroll
         for (int b = 0; b < NJ; b++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) part[wave][a * NJ + b][(g * 4 + i) * 16 + r16] = acc[a][b][i];
+            for (int i = 0; i < 4; i++) sh.part[wave][a * NJ + b][(g * 4 + i) * 16 + r16] = acc[a][b][i];
     __syncthreads();
-    for (uint32_t e = t; e < MF * 16 * NJ * 16; e += 512) {
+    const uint32_t outs = min(A.M, 16u * MF) * 16 * NJ;
+    for (uint32_t e = t; e < outs; e += 512) {
         const uint32_t m = e / (16 * NJ), j = e % (16 * NJ);
-        if (m >= A.M || j >= cols) continue;
+        if (j >= cols) continue;
         float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; k++) v += part[k][m / 16 * NJ + j / 16][m % 16 * 16 + j % 16];
+        for (int k = 0; k < 8; k++) v += sh.part[k][m / 16 * NJ + j / 16][m % 16 * 16 + j % 16];
         store_one(A.c, A.c_type, m * A.ldc + j0 + j, v);
     }
 }
 
-template <int LEFT, int MF> void launch_rows(const RowArgs& R, hipStream_t st) {
+template <int LEFT, int MF, bool FEW> void launch_rows(const RowArgs& R, hipStream_t st) {
     const uint64_t tiles = (R.outer + 15) / 16;
-    if (tiles >= 512) hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 2>), dim3((uint32_t)((tiles + 1) / 2)), dim3(512), 0, st, R);
-    else hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 1>), dim3((uint32_t)tiles), dim3(512), 0, st, R);
+    if (tiles >= 512) hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 2, FEW>), dim3((uint32_t)((tiles + 1) / 2)), dim3(512), 0, st, R);
+    else hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 1, FEW>), dim3((uint32_t)tiles), dim3(512), 0, st, R);
 }
 
 template <int LEFT> hipError_t launch_rows(const RowArgs& R, hipStream_t st) {
-    if (R.M <= 16) launch_rows<LEFT, 1>(R, st);
-    else if (R.M <= 32) launch_rows<LEFT, 2>(R, st);
-    else launch_rows<LEFT, 4>(R, st);
+    if (R.M <= 4) launch_rows<LEFT, 1, true>(R, st);
+    else if (R.M <= 16) launch_rows<LEFT, 1, false>(R, st);
+    else if (R.M <= 32) launch_rows<LEFT, 2, false>(R, st);
+    else launch_rows<LEFT, 4, false>(R, st);
     return hipGetLastError();
 }
 
