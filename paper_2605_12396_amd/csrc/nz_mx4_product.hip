@@ -43,13 +43,15 @@ struct TileArgs {
     uint32_t terms, per_term;                             // linear, grad: bf16 terms of a float; 2^31 over that, upwards
     uint32_t steps;                                       // terms counted
     uint32_t tiles_m, tiles_j;
+    uint32_t parts;                                       // of the length, each a workgroup's; more than one: sums go to `sums`, M rows of
+    float* sums; uint64_t sum_pitch;                      // sum_pitch floats for each part
     void* c; uint64_t ldc; int c_type;
 };
 
 // Which tile: neighbouring workgroups go to the 8 XCDs in turn, so each XCD is given a contiguous run of tiles; in it, bands of 8 tiles of
 // m are walked along j, so that the 32 tiles that an XCD works on at a time share a few panels of either side in its L2.
 __device__ inline void tile_of(const TileArgs& A, uint32_t& tm, uint32_t& tj) {
-    const uint32_t total = A.tiles_m * A.tiles_j, id = blockIdx.x;
+    const uint32_t total = A.tiles_m * A.tiles_j, id = blockIdx.x % total;
     const uint32_t q = total / 8, r = total % 8, x = id % 8;
     const uint32_t t = x * q + min(x, r) + id / 8;
     const uint32_t band = t / (8 * A.tiles_j), first = band * 8;
@@ -94,6 +96,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     uint32_t t, lane, wave, g, l32, wm, wj, rows, cols, nb;
     uint64_t m0, j0;
     const uint8_t *left, *right, *left_s, *right_s;
+    uint32_t part, first, steps;                                       // this workgroup's steps: from `first` to below `steps`
     uint32_t lo[LL], ro[RL ? RL : 1], slo[SL ? SL : 1], sro[SR ? SR : 1];
     uint32_t lchunk;
     uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1, columns PW gq .. of a piece
@@ -105,6 +108,9 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         tile_of(A, tm, tj);
         tm = __builtin_amdgcn_readfirstlane(tm); tj = __builtin_amdgcn_readfirstlane(tj);      // (the same in all lanes anyway)
         m0 = (uint64_t)tm * BM; j0 = (uint64_t)tj * BN;
+        part = __builtin_amdgcn_readfirstlane(blockIdx.x / (A.tiles_m * A.tiles_j));
+        first = (uint32_t)((uint64_t)A.steps * part / A.parts); steps = (uint32_t)((uint64_t)A.steps * (part + 1) / A.parts);
+        first = __builtin_amdgcn_readfirstlane(first); steps = __builtin_amdgcn_readfirstlane(steps);
         t = threadIdx.x; lane = t % 64; wave = __builtin_amdgcn_readfirstlane(t / 64);
         g = lane / 32; l32 = lane % 32;
         wm = wave / WN * (BM / WM); wj = wave % WN * (BN / WN);
@@ -139,8 +145,8 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     __device__ __forceinline__ void fetch(uint32_t s, Half* __restrict h) {
         const uint32_t rs = right_step(s);
         const rsrc_t bl = buffer_at(left + (uint64_t)s * 128);
-        const bool on = s < A.steps;
-        const bool in = OP == PRODUCT ? s * 8 + lchunk < nb : on & ((A.terms > 1) | ((uint64_t)rs * 64 + lchunk * 8 < A.inner));
+        const bool on = s < steps;
+        const bool in = OP == PRODUCT ? on & (s * 8 + lchunk < nb) : on & ((A.terms > 1) | ((uint64_t)rs * 64 + lchunk * 8 < A.inner));
 #pragma unroll
         for (int i = 0; i < LL; i++) load_lds<16>(bl, h->l + (i * NT + wave * 64) * 16, in ? lo[i] : kNowhere);
         if (OP == GRAD) {
@@ -165,14 +171,14 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     __device__ __forceinline__ void fetch_rest(uint32_t s, Half* __restrict h) {
         if constexpr (OP != GRAD) {
             const uint32_t rs = right_step(s);
-            const bool on = s < A.steps;
+            const bool on = s < steps;
             const rsrc_t br = buffer_at(right + (uint64_t)rs * RB);
-            const bool r_in = OP == PRODUCT ? s * 8 + lchunk < nb : on & (rs * 2 + (t % 2 ^ t / 16 % 2) < nb);
+            const bool r_in = OP == PRODUCT ? on & (s * 8 + lchunk < nb) : on & (rs * 2 + (t % 2 ^ t / 16 % 2) < nb);
 #pragma unroll
             for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, r_in ? ro[i] : kNowhere);
             if (OP == PRODUCT) {
                 const rsrc_t bsl = buffer_at(left_s + (uint64_t)s * 8), bsr = buffer_at(right_s + (uint64_t)s * 8);
-                const bool s_in = s * 8 + t % 2 * 4 < nb;
+                const bool s_in = on & (s * 8 + t % 2 * 4 < nb);
 #pragma unroll
                 for (int i = 0; i < SL; i++) load_lds<4>(bsl, h->sl + (i * NT + wave * 64) * 4, s_in ? slo[i] : kNowhere);
 #pragma unroll
@@ -321,15 +327,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 
     // The wave's part of C, 32 rows at a time, through a part of a half's memory: a lane holds 4 neighbouring columns of a row (the right is
     // the matrix instructions' first operand), and leaves with 16 bytes of a row next to those of its neighbours.
-    template <typename T> __device__ __forceinline__ void store(uint8_t* scratch, const f32x16 (&acc)[TM][TN]) {
+    template <typename T> __device__ __forceinline__ void store(void* to, uint64_t ld, uint8_t* scratch, const f32x16 (&acc)[TM][TN]) {
         typedef T t4 __attribute__((ext_vector_type(4)));
         constexpr int B = out_tiles(sizeof(T));
         static_assert(B >= 1 && TN % B == 0, "");
         constexpr uint32_t W = B * 32, E = 16 / sizeof(T);             // columns of a pass; elements of 16 bytes
         constexpr uint32_t P = out_bytes(B, sizeof(T));
         uint8_t* const mine = scratch + wave * 32 * P;
-        const rsrc_t rc = buffer_at(reinterpret_cast<T*>(A.c) + m0 * A.ldc + j0);
-        const uint32_t pitch = (uint32_t)A.ldc * (uint32_t)sizeof(T);
+        const rsrc_t rc = buffer_at(reinterpret_cast<T*>(to) + m0 * ld + j0);
+        const uint32_t pitch = (uint32_t)ld * (uint32_t)sizeof(T);
         const bool wide = pitch % 16 == 0;
 #pragma unroll
         for (int a = 0; a < TM; a++)
@@ -382,27 +388,28 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     for (int a = 0; a < Tl::TM; a++)
 #pragma unroll
         for (int b = 0; b < Tl::TN; b++) acc[a][b] = f32x16{};
-    T.fetch(0, &h0);
-    T.fetch_rest(0, &h0);
+    uint32_t s = T.first;
+    T.fetch(s, &h0);
+    T.fetch_rest(s, &h0);
     T.turn(&h0);
-    T.fetch(1, &h1);
+    T.fetch(s + 1, &h1);
     T.meet();
     typename Tl::Frag F;
     typename Tl::Side S;
-    T.load_side(0, &h0, S);
+    T.load_side(s, &h0, S);
     T.load_frag(0, &h0, F);
     T.template widen<0>(S, F);
-    uint32_t s = 0;
-    for (; s + 1 < A.steps; s += 2) {
+    for (; s + 1 < T.steps; s += 2) {
         T.step(s, &h0, &h1, F, S, acc);
         T.step(s + 1, &h1, &h0, F, S, acc);
     }
-    if (s < A.steps) T.step(s, &h0, &h1, F, S, acc);
+    if (s < T.steps) T.step(s, &h0, &h1, F, S, acc);
     Tl::meet();                                                        // (nor may a load reach shared memory after the workgroup's end)
     uint8_t* const scratch = reinterpret_cast<uint8_t*>(&h0);
-    if (A.c_type == F32) T.template store<float>(scratch, acc);
-    else if (A.c_type == BF16) T.template store<__bf16>(scratch, acc);
-    else T.template store<_Float16>(scratch, acc);
+    if (A.parts > 1) T.template store<float>(A.sums + T.part * A.M * A.sum_pitch, A.sum_pitch, scratch, acc);
+    else if (A.c_type == F32) T.template store<float>(A.c, A.ldc, scratch, acc);
+    else if (A.c_type == BF16) T.template store<__bf16>(A.c, A.ldc, scratch, acc);
+    else T.template store<_Float16>(A.c, A.ldc, scratch, acc);
 }
 
 // A float as bf16 terms that add up to it: one for bf16, two for fp16 (11 bits), three for float32 (24 bits).  Each term takes the top of
@@ -519,16 +526,20 @@ __device__ __forceinline__ void store_one(void* c, int type, uint64_t at, float 
 // left, which serves all NJ tiles of 16 columns.  LEFT: type of the floats (then a unit is four matrix instructions a term, lane group
 // g = lane / 16 taking elements 32 g + 8 j .. + 7 in the j-th; rows start at multiples of 16 bytes and have a multiple of 8 elements), or -1
 // for four bits (one instruction, group g taking block g).
-// The matrix instructions take 16 rows whether there are as many or not.  FEW: up to 4 rows, which also come through shared memory, each
-// byte loaded once; else every lane loads the fragments that it multiplies.
+// The matrix instructions take 16 rows whether there are as many or not.  FEW: as many rows as few_rows says, which also come through shared
+// memory, each byte loaded and cut into terms once; else every lane loads the fragments that it multiplies, and the next units' codes are on
+// their way meanwhile (FEW has two workgroups on a compute unit instead).
+__host__ __device__ constexpr uint32_t few_rows(int left) { return left < 0 ? 4 : left == F32 ? 1 : left == F16 ? 2 : 4; }
+
 template <int LEFT, int MF, int NJ, bool FEW>
 __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
     constexpr int T = LEFT < 0 ? BF16 : LEFT;
     constexpr int terms = terms_of(T);
-    constexpr int S = LEFT < 0 ? (MF == 4 ? 4 : 8) : FEW ? (T == F32 ? 4 : 8) : MF * terms >= 8 ? 1 : MF * terms >= 3 ? 2 : MF * terms == 2 ? 4 : 8;
+    constexpr int S = FEW ? 8 : LEFT < 0 ? 4 : MF * terms >= 6 ? 1 : MF * terms >= 2 ? 2 : 4;
     constexpr uint32_t LB = LEFT < 0 ? S * 64 : S * 128 * float_bytes(T);                     // bytes of a row of the left and S units
-    constexpr uint32_t kScaleWords = 16 * NJ * S, kLeftBytes = FEW ? 4 * LB : 0, kLeftScales = FEW && LEFT < 0 ? 4 * S * 4 : 0;
-    struct Own { uint8_t left[kLeftBytes + 16]; uint32_t scales[kScaleWords]; uint32_t left_scales[kLeftScales / 4 + 4]; };
+    constexpr uint32_t kScaleWords = 16 * NJ * S, FR = few_rows(LEFT);
+    constexpr uint32_t RowB = LEFT < 0 ? LB : S * 256;                                        // of a row and term in shared memory
+    struct Own { uint8_t left[FEW ? FR * terms * RowB : 16]; uint32_t scales[kScaleWords]; uint32_t left_scales[FEW && LEFT < 0 ? FR * S : 4]; };
     union Shared { Own own[8]; float part[8][MF * NJ][256]; };
     __shared__ __attribute__((aligned(16))) Shared sh;
     const uint32_t t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), r16 = lane % 16, g = lane / 16;
@@ -553,46 +564,55 @@ __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
         lso[a] = m * (uint32_t)A.left_spitch;
     }
 
-    for (uint32_t u = u0; u < u1; u += S) {
+    constexpr uint32_t SW = (kScaleWords + 63) / 64;
+    i32x4 w[S][NJ];
+    uint32_t sw[SW];
+    auto ask = [&](uint32_t u) {                                        // the right's codes, and its scales, a word a unit
         const rsrc_t br = buffer_at(A.right + j0 * A.right_pitch + (uint64_t)u * 64), bs = buffer_at(A.right_scales + j0 * A.right_spitch + (uint64_t)u * 4);
-        const rsrc_t bl = buffer_at(A.left + (uint64_t)u * LB / S), bls = buffer_at(A.left_scales + (uint64_t)u * 4);
-        // the right's codes
-        i32x4 w[S][NJ];
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int b = 0; b < NJ; b++) w[s][b] = load16(br, (u + s < u1) & ((u + s) * 4 + g < nb) ? ro[b] + s * 64 : kNowhere);
-        // its scales, a word a unit
-        constexpr uint32_t SW = (kScaleWords + 63) / 64;
-        uint32_t sw[SW];
+            for (int b = 0; b < NJ; b++) w[s][b] = load16(br, ((u + s < u1) & ((u + s) * 4 + g < nb)) ? ro[b] + s * 64 : kNowhere);
 #pragma unroll
         for (uint32_t i = 0; i < SW; i++) {
             const uint32_t e = i * 64 + lane, row = e / S, un = e % S;
             sw[i] = __builtin_amdgcn_raw_buffer_load_b32(bs, u + un < u1 ? min(row, cols - 1) * (uint32_t)A.right_spitch + un * 4 : kNowhere, 0, 0);
         }
+    };
+    if (!FEW) ask(u0);
+    for (uint32_t u = u0; u < u1; u += S) {
+        const rsrc_t bl = buffer_at(A.left + (uint64_t)u * LB / S), bls = buffer_at(A.left_scales + (uint64_t)u * 4);
+        if (FEW) ask(u);
         // the left
         i32x4 x[FEW ? 1 : S][MF][FEW ? 1 : LEFT < 0 ? 1 : 4 * terms];
         uint32_t xs[S][MF];
         if constexpr (FEW) {
-            constexpr uint32_t LN = kLeftBytes / 1024;                  // (a load of the wave is part of one row or covers whole ones)
-            i32x4 lv[LN];
+            constexpr uint32_t E = LEFT < 0 ? 16 : 8 * float_bytes(T);  // bytes of a lane's piece: a block, or eight floats
+            constexpr uint32_t LN = FR * LB / E / 64;
+            const uint64_t end = LEFT < 0 ? (uint64_t)nb * 16 : A.inner * float_bytes(T);               // bytes of a row
+            Eight<T> lv[LN];
             uint32_t ls = 0;
 #pragma unroll
             for (uint32_t i = 0; i < LN; i++) {
-                const uint32_t e = (i * 64 + lane) * 16, row = e / LB, at = e % LB;
-                const uint64_t end = LEFT < 0 ? (uint64_t)nb * 16 : A.inner * float_bytes(T);           // bytes of a row
+                const uint32_t e = (i * 64 + lane) * E, row = e / LB, at = e % LB;
                 const bool in = (row < A.M) & (u + at / (LB / S) < u1) & ((uint64_t)u * (LB / S) + at < end);
-                lv[i] = load16(bl, in ? row * (uint32_t)A.left_pitch + at : kNowhere);
+                lv[i].load_words(bl, in ? row * (uint32_t)A.left_pitch + at : kNowhere);
             }
             if constexpr (LEFT < 0) {
                 const uint32_t row = lane / S, un = lane % S;
-                ls = __builtin_amdgcn_raw_buffer_load_b32(bls, (row < min(A.M, 4u)) & (u + un < u1) ? row * (uint32_t)A.left_spitch + un * 4 : kNowhere, 0, 0);
+                ls = __builtin_amdgcn_raw_buffer_load_b32(bls, ((row < A.M) & (u + un < u1)) ? row * (uint32_t)A.left_spitch + un * 4 : kNowhere, 0, 0);
             }
 #pragma unroll
-            for (uint32_t i = 0; i < SW; i++) if (kScaleWords % 64 == 0 || i * 64 + lane < kScaleWords) own.scales[i * 64 + lane] = sw[i];
+            for (uint32_t i = 0; i < SW; i++) own.scales[i * 64 + lane] = sw[i];
 #pragma unroll
-            for (uint32_t i = 0; i < LN; i++) *reinterpret_cast<i32x4*>(&own.left[(i * 64 + lane) * 16]) = lv[i];
-            if (LEFT < 0 && lane < 4 * S) own.left_scales[lane] = ls;
+            for (uint32_t i = 0; i < LN; i++) {
+                const uint32_t e = (i * 64 + lane) * 16, row = e / RowB, at = e % RowB;
+                i32x4 v[terms];
+                lv[i].terms(v);
+#pragma unroll
+                for (int q = 0; q < terms; q++) *reinterpret_cast<i32x4*>(&own.left[(row * terms + q) * RowB + at]) = v[q];
+            }
+            if (LEFT < 0 && lane < FR * S) own.left_scales[lane] = ls;
         } else {
 #pragma unroll
             for (int s = 0; s < S; s++)
@@ -619,6 +639,12 @@ __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
 #pragma unroll
             for (uint32_t i = 0; i < SW; i++) if (kScaleWords % 64 == 0 || i * 64 + lane < kScaleWords) own.scales[i * 64 + lane] = sw[i];
         }
+        i32x4 now[S][NJ];
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int b = 0; b < NJ; b++) now[s][b] = w[s][b];
+        if (!FEW) ask(u + S);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
         const uint32_t few = FEW ? min(r16, A.M - 1) : 0;               // this lane's row of the left
@@ -635,10 +661,10 @@ __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
                 for (int a = 0; a < MF; a++) {
                     const uint32_t v = FEW ? (uint32_t)reinterpret_cast<const uint8_t*>(own.left_scales)[(few * S + s) * 4 + g] : __builtin_amdgcn_ubfe(xs[s][a], 8 * g, 8);
                     const uint32_t sa = (u + s) * 4 + g < nb ? v : 0;
-                    const i32x4 p = FEW ? *reinterpret_cast<const i32x4*>(&own.left[few * LB + s * 64 + g * 16]) : x[FEW ? 0 : s][a][0];
+                    const i32x4 p = FEW ? *reinterpret_cast<const i32x4*>(&own.left[few * RowB + s * 64 + g * 16]) : x[FEW ? 0 : s][a][0];
 #pragma unroll
                     for (int b = 0; b < NJ; b++) {
-                        const i32x4 q = w[s][b];
+                        const i32x4 q = now[s][b];
                         const i32x8 p8 = { p[0], p[1], p[2], p[3], 0, 0, 0, 0 }, q8 = { q[0], q[1], q[2], q[3], 0, 0, 0, 0 };
                         acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p8, q8, acc[a][b], 4, 4, 0, sa, 0, sb[b]);
                     }
@@ -647,17 +673,14 @@ __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     i32x4 v[terms];
-                    if constexpr (FEW) {
-                        Eight<T> e;
+                    if constexpr (FEW)
 #pragma unroll
-                        for (uint32_t i = 0; i < float_bytes(T) / 2; i++)
-                            e.w[i] = *reinterpret_cast<const i32x4*>(&own.left[few * LB + (s * 128 + g * 32 + j * 8) * float_bytes(T) + i * 16]);
-                        e.terms(v);
-                    }
+                        for (int q = 0; q < terms; q++)
+                            v[q] = *reinterpret_cast<const i32x4*>(&own.left[(few * terms + q) * RowB + s * 256 + g * 64 + j * 16]);
 #pragma unroll
                     for (int b = 0; b < NJ; b++) {
                         i32x4 y;
-                        unroll4([&](auto B) { y[B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[s][b][j], mx_scale(sb[b]), B.value)); });
+                        unroll4([&](auto B) { y[B.value] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(now[s][b][j], mx_scale(sb[b]), B.value)); });
 #pragma unroll
                         for (int a = 0; a < MF; a++)
 #pragma unroll
@@ -697,31 +720,80 @@ template <int LEFT, int MF, bool FEW> void launch_rows(const RowArgs& R, hipStre
 }
 
 template <int LEFT> hipError_t launch_rows(const RowArgs& R, hipStream_t st) {
-    if (R.M <= 4) launch_rows<LEFT, 1, true>(R, st);
+    if (R.M <= few_rows(LEFT)) launch_rows<LEFT, 1, true>(R, st);
     else if (R.M <= 16) launch_rows<LEFT, 1, false>(R, st);
-    else if (R.M <= 32) launch_rows<LEFT, 2, false>(R, st);
-    else launch_rows<LEFT, 4, false>(R, st);
+    else launch_rows<LEFT, 2, false>(R, st);
     return hipGetLastError();
 }
 
-constexpr uint64_t kFewRows = 64;
+// Rows up to which k_mx_rows is taken.  Against 4096 x 4096 in four bits and with bf16, in microseconds: 32 rows 8.1 and 11.6, by tiles 13.3
+// and 16.4; 64 rows (with room for them in its registers) 11.8 and 19.1, by tiles 13.2 and 18.7, against 8192 x 8192 24.9 and 39.1, by
+// tiles 20.2 and 33.0.
+constexpr uint64_t kFewRows = 32;
 
-template <int OP, int BM, int BN, int WM, int WN> void launch_tile(const TileArgs& T, hipStream_t st) {
-    hipLaunchKernelGGL((k_mx_tile<OP, BM, BN, WM, WN>), dim3(T.tiles_m * T.tiles_j), dim3(64 * WM * WN), 0, st, T);
+// Sums of the parts of a length, in their order, into C: a thread makes four neighbouring columns.
+__global__ __launch_bounds__(256) void k_mx_join(const float* sums, uint32_t parts, uint64_t M, uint64_t outer, uint64_t pitch, void* c, uint64_t ldc, int type) {
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x, per_row = pitch / 4, m = id / per_row, j = id % per_row * 4;
+    if (m >= M) return;
+    f32x4 v = {};
+    for (uint32_t p = 0; p < parts; p++) v += *reinterpret_cast<const f32x4*>(sums + (p * M + m) * pitch + j);
+    for (uint32_t i = 0; i < 4; i++)
+        if (j + i < outer) store_one(c, type, m * ldc + j + i, v[i]);
 }
 
-template <int OP> hipError_t launch_tiles(TileArgs& T, hipStream_t st) {
-    auto count = [&](uint32_t bm, uint32_t bn) {
-        T.tiles_m = (uint32_t)((T.M + bm - 1) / bm); T.tiles_j = (uint32_t)((T.outer + bn - 1) / bn);
-        return T.tiles_m * T.tiles_j;
-    };
-    if (count(256, 256) >= 192) launch_tile<OP, 256, 256, 2, 2>(T, st);
-    else { count(128, 128); launch_tile<OP, 128, 128, 2, 2>(T, st); }
+// How a product is laid over the chip: tiles of 256 x 256, one workgroup to a compute unit, or of 128 x 128, two; and the length in parts,
+// whose sums a second kernel joins, where there are fewer tiles than compute units.  The least of these estimates in microseconds is taken:
+// a step of a tile takes `alone` where few of them run, and `share` more where each compute unit has one (two of 128 x 128: twice
+// that), since all draw on the same caches and the same power.  Measured on 16 to 512 tiles of 4 to 128 steps; one in ten of the choices is
+// up to a tenth slower than the best.  For instance bf16 on the left, 256 rows through 4096 x 4096: tiles of 128 33.1 us and in four parts
+// 25.1, tiles of 256 78.9; 2048 rows through 8192 x 8192: 281.6, of 256 208.5.
+struct Plan { uint32_t tile, parts; };
+struct StepCost { float alone128, share128, alone256, share256; };
+constexpr StepCost kStepCost[3] = { { 0.60f, 0.30f, 1.40f, 0.75f }, { 0.42f, 0.30f, 1.15f, 0.45f }, { 0.80f, 0.25f, 1.45f, 0.28f } };
+
+Plan plan_tiles(int op, uint64_t M, uint64_t outer, uint32_t steps) {
+    Plan best = { 256, 1 };
+    float least = 0.0f;
+    for (uint32_t tile = 128; tile <= 256; tile *= 2) {
+        const float alone = tile == 128 ? kStepCost[op].alone128 : kStepCost[op].alone256;
+        const float share = tile == 128 ? kStepCost[op].share128 : kStepCost[op].share256;
+        const float resident = tile == 128 ? 512.0f : 256.0f;
+        const uint64_t tiles = ((M + tile - 1) / tile) * ((outer + tile - 1) / tile);
+        for (uint32_t parts = 1; parts <= 16 && (parts == 1 || (parts <= steps / 2 && tiles * parts <= 512)); parts++) {
+            const float groups = (float)(tiles * parts), rounds = (float)(uint64_t)((groups + resident - 1.0f) / resident);
+            const float step = alone + share * (groups < resident ? groups : resident) / 256.0f;
+            float us = 6.0f + rounds * (5.0f + step * (float)((steps + parts - 1) / parts));
+            if (parts > 1) us += 3.0f + (float)(parts * M * outer) * 8.0f / 4e6f;      // the joining kernel; its sums written and read
+            if ((tile == 128 && parts == 1) || us < least) { best = { tile, parts }; least = us; }
+        }
+    }
+    return best;
+}
+
+uint64_t sum_pitch(uint64_t outer) { return (outer + 3) / 4 * 4; }
+
+size_t sums_bytes(const Plan& p, uint64_t M, uint64_t outer) { return p.parts > 1 ? (size_t)p.parts * M * sum_pitch(outer) * 4 : 0; }
+
+template <int OP> hipError_t launch_tiles(TileArgs& T, const Plan& p, float* sums, hipStream_t st) {
+    T.tiles_m = (uint32_t)((T.M + p.tile - 1) / p.tile); T.tiles_j = (uint32_t)((T.outer + p.tile - 1) / p.tile);
+    T.parts = p.parts; T.sums = sums; T.sum_pitch = sum_pitch(T.outer);
+    const dim3 grid(T.tiles_m * T.tiles_j * p.parts);
+    if (p.tile == 256) hipLaunchKernelGGL((k_mx_tile<OP, 256, 256, 2, 2>), grid, dim3(256), 0, st, T);
+    else hipLaunchKernelGGL((k_mx_tile<OP, 128, 128, 2, 2>), grid, dim3(256), 0, st, T);
+    if (p.parts > 1)
+        hipLaunchKernelGGL(k_mx_join, dim3((uint32_t)((T.M * (T.sum_pitch / 4) + 255) / 256)), dim3(256), 0, st, sums, p.parts, T.M, T.outer, T.sum_pitch,
+                           T.c, T.ldc, T.c_type);
     return hipGetLastError();
 }
 
 // Whether the matrix instructions can be fed from the caller's rows: bf16, rows and their ends at multiples of 16 bytes.
 bool fed_directly(const MxProductArgs& A, uint64_t inner, int left) { return left == BF16 && A.ldx % 8 == 0 && inner % 8 == 0; }
+
+uint32_t steps_of(int kind, int left, uint64_t inner) {
+    return kind == PRODUCT ? (uint32_t)((inner + 255) / 256) : (uint32_t)((inner + 63) / 64) * terms_of(left);
+}
+
+size_t terms_bytes(int kind, int left, uint64_t M, uint64_t inner) { return kind == PRODUCT ? 0 : (inner + 63) / 64 * 128 * M * terms_of(left); }
 
 template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint32_t chunks, hipStream_t st) {
     hipLaunchKernelGGL((k_mx_terms<T>), dim3((uint32_t)((A.M * chunks * 8 + 255) / 256)), dim3(256), 0, st, reinterpret_cast<const uint8_t*>(A.x), A.ldx,
@@ -731,10 +803,11 @@ template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint3
 }  // namespace
 
 size_t mx_product_workspace(int kind, int left, uint64_t M, uint64_t N, uint64_t K) {
-    if (kind == PRODUCT) return 0;
-    if (kind == LINEAR && M <= kFewRows) return M * ((K + 7) / 8 * 8) * float_bytes(left);
-    const uint64_t inner = kind == GRAD ? N : K;
-    return (inner + 63) / 64 * 128 * M * terms_of(left);
+    const uint64_t inner = kind == GRAD ? N : K, outer = kind == GRAD ? K : N;
+    if (kind != GRAD && M <= kFewRows) return kind == PRODUCT ? 0 : M * ((K + 7) / 8 * 8) * float_bytes(left);
+    // (bf16 may need no terms, but then it has the plan of one term)
+    const Plan p = plan_tiles(kind, M, outer, steps_of(kind, left, inner));
+    return terms_bytes(kind, left, M, inner) + sums_bytes(p, M, outer);
 }
 
 hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStream_t st) {
@@ -766,10 +839,12 @@ hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStre
     T.c = A.c; T.ldc = A.ldc; T.c_type = A.c_type;
     T.right = A.b.codes; T.right_pitch = A.b.pitch * 16; T.right_scales = A.b.scales; T.right_spitch = A.b.pitch;
     T.terms = 1;
+    T.steps = steps_of(kind, left, T.inner);
+    const Plan p = plan_tiles(kind, T.M, T.outer, T.steps);
+    float* const sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(A.ws) + terms_bytes(kind, left, T.M, T.inner));
     if (kind == PRODUCT) {
         T.left = A.a.codes; T.left_pitch = A.a.pitch * 16; T.left_scales = A.a.scales; T.left_spitch = A.a.pitch;
-        T.steps = (uint32_t)((T.inner + 255) / 256);
-        return launch_tiles<PRODUCT>(T, st);
+        return launch_tiles<PRODUCT>(T, p, sums, st);
     }
     const uint32_t chunks = (uint32_t)((T.inner + 63) / 64);
     if (fed_directly(A, T.inner, left)) {
@@ -783,9 +858,8 @@ hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStre
         if (e != hipSuccess) return e;
         T.left = reinterpret_cast<const uint8_t*>(A.ws); T.left_pitch = (uint64_t)chunks * 128 * T.terms;
     }
-    T.steps = chunks * T.terms;
     T.per_term = (0x80000000u + T.terms - 1) / T.terms;
-    return kind == LINEAR ? launch_tiles<LINEAR>(T, st) : launch_tiles<GRAD>(T, st);
+    return kind == LINEAR ? launch_tiles<LINEAR>(T, p, sums, st) : launch_tiles<GRAD>(T, p, sums, st);
 }
 
 }  // namespace nz
