@@ -32,25 +32,35 @@ __device__ inline uint32_t blocks_here(const MxRows& R) {
     return (uint32_t)(left < R.group ? left : R.group) * R.nb;
 }
 
-template <int T> __device__ inline float as_float(uint16_t v) {
-    if (T == BF16) return __uint_as_float((uint32_t)v << 16);
-    return (float)__builtin_bit_cast(_Float16, v);
+// 16 bytes at any address that suits their elements: rows may start anywhere, and the memory pipeline splits what crosses a line.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 __attribute__((aligned(4))) u32x4_by4;
+typedef u32x4 __attribute__((aligned(2))) u32x4_by2;
+template <int T> struct Words { typedef u32x4_by2 type; };
+template <> struct Words<F32> { typedef u32x4_by4 type; };
+
+template <int T> __device__ inline float as_float(uint32_t v) {
+    if (T == BF16) return __uint_as_float(v << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)v);
 }
 
 // Eight floats of a row from column c on; those past the row's end are 0.
-template <int T> __device__ inline void load8(const void* in, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, bool wide, float* x) {
+template <int T> __device__ inline void load8(const void* in, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, float* x) {
     constexpr uint32_t sz = float_bytes(T);
     const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + (row * ld + c) * sz;
-    if (wide && c + 8 <= cols) {
+    if (c + 8 <= cols) {
+        const typename Words<T>::type* w = reinterpret_cast<const typename Words<T>::type*>(p);
+        const u32x4 u = w[0];
         if (T == F32) {
-            const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
-            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            const u32x4 v = w[1];
+#pragma unroll
+            for (int i = 0; i < 4; i++) { x[i] = __uint_as_float(u[i]); x[4 + i] = __uint_as_float(v[i]); }
         } else {
-            const uint4 u = reinterpret_cast<const uint4*>(p)[0];
-            const uint32_t w[4] = { u.x, u.y, u.z, u.w };
-            for (int i = 0; i < 4; i++) { x[2 * i] = as_float<T>((uint16_t)w[i]); x[2 * i + 1] = as_float<T>((uint16_t)(w[i] >> 16)); }
+#pragma unroll
+            for (int i = 0; i < 4; i++) { x[2 * i] = as_float<T>(u[i] & 0xFFFFu); x[2 * i + 1] = as_float<T>(u[i] >> 16); }
         }
     } else {
+#pragma unroll
         for (int i = 0; i < 8; i++) {
             if (T == F32) x[i] = c + i < cols ? reinterpret_cast<const float*>(p)[i] : 0.0f;
             else x[i] = c + i < cols ? as_float<T>(reinterpret_cast<const uint16_t*>(p)[i]) : 0.0f;
@@ -63,25 +73,19 @@ template <int T> __device__ inline uint32_t to16(float v) {
     return __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-template <int T> __device__ inline void store8(void* out, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, bool wide, const float* x) {
+// N floats, packed in w, of a row from column c on; those past the row's end are left alone.
+template <int T, int N> __device__ inline void store_words(void* out, uint64_t row, uint64_t ld, uint64_t c, uint64_t cols, u32x4 w) {
     constexpr uint32_t sz = float_bytes(T);
+    static_assert(N * sz == 16, "");
     uint8_t* p = reinterpret_cast<uint8_t*>(out) + (row * ld + c) * sz;
-    if (wide && c + 8 <= cols) {
-        if (T == F32) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-            uint32_t w[4];
-            for (int i = 0; i < 4; i++) w[i] = to16<T>(x[2 * i]) | to16<T>(x[2 * i + 1]) << 16;
-            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    } else {
-        for (int i = 0; i < 8; i++)
+    if (c + N <= cols) *reinterpret_cast<typename Words<T>::type*>(p) = w;
+    else
+#pragma unroll
+        for (int i = 0; i < N; i++)
             if (c + i < cols) {
-                if (T == F32) reinterpret_cast<float*>(p)[i] = x[i];
-                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)to16<T>(x[i]);
+                if (T == F32) reinterpret_cast<uint32_t*>(p)[i] = w[i % 4];
+                else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2 % 4] >> (i % 2 * 16));
             }
-    }
 }
 
 // The largest of four neighbouring lanes' values.
@@ -153,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxConvertArgs A) {
     float x[kOctets][8];
     for (uint32_t u = 0; u < kOctets; u++) {
         p[u] = place(A.R, first + u * kThreads, limit);
-        if (p[u].live) load8<T>(A.in, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, A.wide, x[u]);
+        if (p[u].live) load8<T>(A.in, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, x[u]);
     }
     for (uint32_t u = 0; u < kOctets; u++) {
         if (!p[u].live) continue;                     // (all four lanes of a block)
@@ -165,32 +169,90 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxConvertArgs A) {
     }
 }
 
-// OUT: the floats' type, or -1 for four bits.
-template <int OUT, bool SR>
-__global__ __launch_bounds__(kThreads) void k_mx_sum(MxSumArgs A) {
+// OUT: the floats' type, or -1 for four bits.  MAX: the most operands; up to kMxSomeOperands of them are asked for at once.
+template <int OUT, bool SR, uint32_t MAX>
+__global__ __launch_bounds__(kThreads) void k_mx_sum(MxSumArgs<MAX> A) {
     const uint32_t limit = blocks_here(A.R);
-    const Place p = place(A.R, blockIdx.x * kThreads + threadIdx.x, limit);
-    if (!p.live) return;
-    const uint64_t c = p.blk * 32ull + p.q * 8u;
-    float acc[8], x[8];
-    for (uint32_t i = 0; i < A.k; i++) {
-        const uint64_t at = p.row * A.in[i].pitch + p.blk;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(A.in[i].codes + at * 16 + p.q * 4);
-        decode8(w, A.in[i].scales[at], x);
-        for (int j = 0; j < 8; j++) acc[j] = i ? acc[j] + x[j] : x[j];
+    constexpr uint32_t U = MAX > 1 ? 2 : 4;                               // octets of a thread
+    constexpr uint32_t G = MAX < kMxSomeOperands ? MAX : kMxSomeOperands;
+    const uint32_t first = blockIdx.x * (kThreads * U) + threadIdx.x;
+    Place p[U];
+    float acc[U][8];
+#pragma unroll
+    for (uint32_t u = 0; u < U; u++) p[u] = place(A.R, first + u * kThreads, limit);
+    for (uint32_t i0 = 0; i0 < A.k; i0 += G) {
+        uint32_t w[G][U], s[G][U];
+#pragma unroll
+        for (uint32_t i = 0; i < G; i++)
+            if (i0 + i < A.k)
+#pragma unroll
+                for (uint32_t u = 0; u < U; u++)
+                    if (p[u].live) {
+                        const uint64_t at = p[u].row * A.in[i0 + i].pitch + p[u].blk;
+                        w[i][u] = *reinterpret_cast<const uint32_t*>(A.in[i0 + i].codes + at * 16 + p[u].q * 4);
+                        s[i][u] = A.in[i0 + i].scales[at];
+                    }
+#pragma unroll
+        for (uint32_t i = 0; i < G; i++)
+            if (i0 + i < A.k)
+#pragma unroll
+                for (uint32_t u = 0; u < U; u++) {
+                    float x[8];
+                    decode8(w[i][u], s[i][u], x);
+#pragma unroll
+                    for (int j = 0; j < 8; j++) acc[u][j] = i0 + i ? acc[u][j] + x[j] : x[j];
+                }
     }
-    if (A.local) {
-        load8<F32>(A.local, p.row, A.ld_local, c, A.R.cols, A.local_wide, x);
-        for (int j = 0; j < 8; j++) acc[j] += x[j];
-    }
-    if (OUT >= 0) {
-        store8<OUT < 0 ? F32 : OUT>(A.out, p.row, A.ld, c, A.R.cols, A.wide, acc);
+    if (A.local)
+#pragma unroll
+        for (uint32_t u = 0; u < U; u++)
+            if (p[u].live) {
+                float x[8];
+                load8<F32>(A.local, p[u].row, A.ld_local, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, x);
+#pragma unroll
+                for (int j = 0; j < 8; j++) acc[u][j] += x[j];
+            }
+    if constexpr (OUT == F32) {
+        // a lane's eight floats are 32 bytes; exchanged through shared memory, a wave's stores are of 16 bytes next to each other
+        __shared__ __attribute__((aligned(16))) u32x4 turn[kThreads * 2];
+        u32x4* const mine = turn + threadIdx.x / 64 * 128;
+        const uint32_t lane = threadIdx.x % 64;
+#pragma unroll
+        for (uint32_t u = 0; u < U; u++) {
+#pragma unroll
+            for (uint32_t h = 0; h < 2; h++) {
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = __float_as_uint(acc[u][h * 4 + j]);
+                mine[(lane * 2 + h) ^ (lane / 8 & 1)] = v;                 // (so that 16 lanes use all banks)
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (uint32_t h = 0; h < 2; h++) {
+                const uint32_t c = h * 64 + lane;                         // quarter c % 2 of the octet of lane c / 2
+                const u32x4 v = mine[c ^ (c / 16 & 1)];
+                const Place o = place(A.R, first - lane + u * kThreads + c / 2, limit);
+                if (o.live) store_words<F32, 4>(A.out, o.row, A.ld, o.blk * 32ull + o.q * 8u + c % 2 * 4, A.R.cols, v);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
     } else {
-        uint32_t s;
-        const uint32_t w = encode8<SR>(acc, (p.row * A.R.nb + p.blk) * 4 + p.q, A.seed, s);
-        const uint64_t at = p.row * A.pitch + p.blk;
-        *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p.q * 4) = w;
-        if (p.q == 0) A.scales[at] = (uint8_t)s;
+#pragma unroll
+        for (uint32_t u = 0; u < U; u++) {
+            if (!p[u].live) continue;
+            if constexpr (OUT >= 0) {
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; j++) v[j] = to16<OUT>(acc[u][2 * j]) | to16<OUT>(acc[u][2 * j + 1]) << 16;
+                store_words<OUT, 8>(A.out, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, v);
+            } else {
+                uint32_t s;
+                const uint32_t w = encode8<SR>(acc[u], (p[u].row * A.R.nb + p[u].blk) * 4 + p[u].q, A.seed, s);
+                const uint64_t at = p[u].row * A.pitch + p[u].blk;
+                *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p[u].q * 4) = w;
+                if (p[u].q == 0) A.scales[at] = (uint8_t)s;
+            }
+        }
     }
 }
 
@@ -213,14 +275,17 @@ hipError_t launch_mx_quantize(const MxConvertArgs& A, int type, bool sr, hipStre
     return hipGetLastError();
 }
 
-hipError_t launch_mx_sum(const MxSumArgs& A, int type, bool sr, hipStream_t st) {
-    const dim3 g = grid_of(A.R, 1), t(kThreads);
-    if (type == F32) hipLaunchKernelGGL((k_mx_sum<F32, false>), g, t, 0, st, A);
-    else if (type == BF16) hipLaunchKernelGGL((k_mx_sum<BF16, false>), g, t, 0, st, A);
-    else if (type == F16) hipLaunchKernelGGL((k_mx_sum<F16, false>), g, t, 0, st, A);
-    else if (sr) hipLaunchKernelGGL((k_mx_sum<-1, true>), g, t, 0, st, A);
-    else hipLaunchKernelGGL((k_mx_sum<-1, false>), g, t, 0, st, A);
+template <uint32_t MAX> hipError_t launch_mx_sum(const MxSumArgs<MAX>& A, int type, bool sr, hipStream_t st) {
+    const dim3 g = grid_of(A.R, MAX > 1 ? 2 : 4), t(kThreads);
+    if (type == F32) hipLaunchKernelGGL((k_mx_sum<F32, false, MAX>), g, t, 0, st, A);
+    else if (type == BF16) hipLaunchKernelGGL((k_mx_sum<BF16, false, MAX>), g, t, 0, st, A);
+    else if (type == F16) hipLaunchKernelGGL((k_mx_sum<F16, false, MAX>), g, t, 0, st, A);
+    else if (sr) hipLaunchKernelGGL((k_mx_sum<-1, true, MAX>), g, t, 0, st, A);
+    else hipLaunchKernelGGL((k_mx_sum<-1, false, MAX>), g, t, 0, st, A);
     return hipGetLastError();
 }
+template hipError_t launch_mx_sum<1>(const MxSumArgs<1>&, int, bool, hipStream_t);
+template hipError_t launch_mx_sum<kMxSomeOperands>(const MxSumArgs<kMxSomeOperands>&, int, bool, hipStream_t);
+template hipError_t launch_mx_sum<kMxMaxOperands>(const MxSumArgs<kMxMaxOperands>&, int, bool, hipStream_t);
 
 }  // namespace nz

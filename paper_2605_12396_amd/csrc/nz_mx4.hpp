@@ -8,7 +8,7 @@ enum : int { F32 = 0, BF16 = 1, F16 = 2 };
 __host__ __device__ constexpr uint32_t float_bytes(int type) { return type == F32 ? 4u : 2u; }
 
 constexpr uint32_t kMxBlock = 32;                 // elements under one scale
-constexpr uint32_t kMxMaxOperands = 64;
+constexpr uint32_t kMxMaxOperands = 64, kMxSomeOperands = 8;
 
 struct MxMat { const uint8_t* codes; const uint8_t* scales; uint64_t pitch; };
 
@@ -26,14 +26,14 @@ struct MxConvertArgs {
     const void* in; uint64_t ld;
     uint8_t* codes; uint8_t* scales; uint64_t pitch;
     uint32_t seed;
-    bool wide;                // rows of `in` start at multiples of 16 bytes
 };
 
-struct MxSumArgs {
+// MAX: room for operands.  Arguments are copied to the GPU with every launch, so few operands do not carry room for many.
+template <uint32_t MAX> struct MxSumArgs {
     MxRows R;
-    MxMat in[kMxMaxOperands]; uint32_t k;
-    const float* local; uint64_t ld_local; bool local_wide;
-    void* out; uint64_t ld; bool wide;                                    // floats
+    MxMat in[MAX]; uint32_t k;
+    const float* local; uint64_t ld_local;
+    void* out; uint64_t ld;                                               // floats
     uint8_t* codes; uint8_t* scales; uint64_t pitch; uint32_t seed;      // or four bits
 };
 
@@ -47,7 +47,7 @@ struct MxProductArgs {
 
 hipError_t launch_mx_quantize(const MxConvertArgs& A, int type, bool stochastic, hipStream_t st);
 // type: of the floats that are written, or -1 for four bits
-hipError_t launch_mx_sum(const MxSumArgs& A, int type, bool stochastic, hipStream_t st);
+template <uint32_t MAX> hipError_t launch_mx_sum(const MxSumArgs<MAX>& A, int type, bool stochastic, hipStream_t st);
 
 size_t mx_product_workspace(int kind, int left, uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStream_t st);

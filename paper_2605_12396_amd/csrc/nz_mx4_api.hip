@@ -26,9 +26,6 @@ bool shape_ok(uint64_t rows, uint64_t cols) {
     return rows > 0 && cols > 0 && rows < kMaxSide && cols < kMaxSide && rows * cols < kMaxElements;
 }
 
-// Rows of floats that start at multiples of 16 bytes (the first one does).
-bool wide_rows(uint64_t rows, uint64_t ld, int type) { return rows == 1 || ld * float_bytes(type) % 16 == 0; }
-
 // Division of a block's number b, below 2^29, by nb as a multiplication: with l = ceil(log2 nb) and m = floor(2^(29 + l) / nb) + 1, m nb
 // exceeds 2^(29 + l) by at most nb <= 2^l, so that b m / 2^(29 + l) exceeds b / nb by less than 1 / nb and has the same whole part.
 MxRows rows_of(uint64_t rows, uint64_t cols) {
@@ -53,19 +50,31 @@ bool operands_ok(const nz_mx4_matrix* in, uint32_t k, const float* d_local, uint
     return !d_local || floats_ok(d_local, NZ_F32, rows, cols, ld_local);
 }
 
-// The arguments of a sum that do not depend on what becomes of it; `gap` says whether its output has gaps between its rows.
-MxSumArgs sum_args(const nz_mx4_matrix* in, uint32_t k, const float* d_local, uint64_t ld_local, uint64_t rows, uint64_t cols, bool gap) {
-    MxSumArgs A = {};
+// What becomes of a sum: floats of `type`, or four bits (type -1).
+struct Outcome { int type; void* out; uint64_t ld; uint8_t *codes, *scales; uint64_t pitch; bool stochastic; uint32_t seed; };
+
+template <uint32_t MAX> nz_status sum_to(const nz_mx4_matrix* in, uint32_t k, const float* d_local, uint64_t ld_local, uint64_t rows, uint64_t cols,
+                                         const Outcome& O, void* stream) {
+    MxSumArgs<MAX> A;
     const uint64_t nb = (cols + 31) / 32;
-    bool flat = one_row(rows, cols) && !gap && (!d_local || ld_local == cols);
+    bool flat = one_row(rows, cols) && (O.type < 0 ? O.pitch == nb : O.ld == cols) && (!d_local || ld_local == cols);
     for (uint32_t i = 0; i < k; i++) {
         A.in[i] = { reinterpret_cast<const uint8_t*>(in[i].codes), reinterpret_cast<const uint8_t*>(in[i].scales), in[i].pitch };
         flat = flat && in[i].pitch == nb;
     }
     A.R = flat ? rows_of(1, rows * cols) : rows_of(rows, cols);
     A.k = k;
-    A.local = d_local; A.ld_local = ld_local; A.local_wide = wide_rows(A.R.rows, ld_local, F32);
-    return A;
+    A.local = d_local; A.ld_local = ld_local;
+    A.out = O.out; A.ld = O.ld;
+    A.codes = O.codes; A.scales = O.scales; A.pitch = O.pitch; A.seed = O.seed;
+    return launch_mx_sum<MAX>(A, O.type, O.stochastic, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? NZ_OK : NZ_ERR_HIP;
+}
+
+nz_status sum_to(const nz_mx4_matrix* in, uint32_t k, const float* d_local, uint64_t ld_local, uint64_t rows, uint64_t cols, const Outcome& O,
+                 void* stream) {
+    if (k == 1) return sum_to<1>(in, k, d_local, ld_local, rows, cols, O, stream);
+    if (k <= kMxSomeOperands) return sum_to<kMxSomeOperands>(in, k, d_local, ld_local, rows, cols, O, stream);
+    return sum_to<kMxMaxOperands>(in, k, d_local, ld_local, rows, cols, O, stream);
 }
 
 bool product_shape_ok(uint64_t M, uint64_t N, uint64_t K) {
@@ -105,7 +114,7 @@ nz_status nz_mx4_quantize(const void* d_in, nz_float_type type, size_t rows, siz
     MxConvertArgs A;
     const bool flat = one_row(rows, cols) && ld == cols && out->pitch == cols / 32;
     A.R = flat ? rows_of(1, rows * cols) : rows_of(rows, cols);
-    A.in = d_in; A.ld = ld; A.wide = wide_rows(A.R.rows, ld, type);
+    A.in = d_in; A.ld = ld;
     A.codes = reinterpret_cast<uint8_t*>(out->codes); A.scales = reinterpret_cast<uint8_t*>(out->scales); A.pitch = out->pitch;
     A.seed = seed;
     const hipError_t e = launch_mx_quantize(A, type, rounding == NZ_MX4_STOCHASTIC, reinterpret_cast<hipStream_t>(stream));
@@ -115,9 +124,8 @@ nz_status nz_mx4_quantize(const void* d_in, nz_float_type type, size_t rows, siz
 nz_status nz_mx4_sum_k(const nz_mx4_matrix* in, uint32_t k, const float* d_local, size_t ld_local, size_t rows, size_t cols,
                        void* d_out, nz_float_type type, size_t ld, void* stream) {
     if (!operands_ok(in, k, d_local, ld_local, rows, cols) || !floats_ok(d_out, type, rows, cols, ld)) return NZ_ERR_INVALID;
-    MxSumArgs A = sum_args(in, k, d_local, ld_local, rows, cols, ld != cols);
-    A.out = d_out; A.ld = ld; A.wide = wide_rows(A.R.rows, ld, type);
-    return launch_mx_sum(A, type, false, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? NZ_OK : NZ_ERR_HIP;
+    const Outcome O = { type, d_out, ld, nullptr, nullptr, 0, false, 0 };
+    return sum_to(in, k, d_local, ld_local, rows, cols, O, stream);
 }
 
 nz_status nz_mx4_dequantize(const nz_mx4_matrix* in, size_t rows, size_t cols, void* d_out, nz_float_type type, size_t ld,
@@ -128,11 +136,9 @@ nz_status nz_mx4_dequantize(const nz_mx4_matrix* in, size_t rows, size_t cols, v
 nz_status nz_mx4_reduce_k(const nz_mx4_matrix* in, uint32_t k, const float* d_local, size_t ld_local, size_t rows, size_t cols,
                           nz_mx4_rounding rounding, uint32_t seed, const nz_mx4_matrix* out, void* stream) {
     if (!operands_ok(in, k, d_local, ld_local, rows, cols) || !is_rounding(rounding) || !matrix_ok(out, rows, cols)) return NZ_ERR_INVALID;
-    MxSumArgs A = sum_args(in, k, d_local, ld_local, rows, cols, out->pitch != (cols + 31) / 32);
-    A.codes = reinterpret_cast<uint8_t*>(out->codes); A.scales = reinterpret_cast<uint8_t*>(out->scales); A.pitch = out->pitch;
-    A.seed = seed;
-    const hipError_t e = launch_mx_sum(A, -1, rounding == NZ_MX4_STOCHASTIC, reinterpret_cast<hipStream_t>(stream));
-    return e == hipSuccess ? NZ_OK : NZ_ERR_HIP;
+    const Outcome O = { -1, nullptr, 0, reinterpret_cast<uint8_t*>(out->codes), reinterpret_cast<uint8_t*>(out->scales), out->pitch,
+                        rounding == NZ_MX4_STOCHASTIC, seed };
+    return sum_to(in, k, d_local, ld_local, rows, cols, O, stream);
 }
 
 size_t nz_mx4_workspace_bytes(nz_mx4_kind kind, nz_float_type left, size_t M, size_t N, size_t K) {
