@@ -32,6 +32,9 @@ __device__ inline uint32_t blocks_here(const MxRows& R) {
     return (uint32_t)(left < R.group ? left : R.group) * R.nb;
 }
 
+// Octets of the rows before this group's.
+__device__ inline uint64_t octets_before(const MxRows& R) { return (uint64_t)blockIdx.y * R.group * R.nb * 4; }
+
 // 16 bytes at any address that suits their elements: rows may start anywhere, and the memory pipeline splits what crosses a line.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 __attribute__((aligned(4))) u32x4_by4;
@@ -94,21 +97,40 @@ __device__ inline uint32_t max_of_four(uint32_t v) {
     return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
 }
 
-// One element, stochastically: its code, given its magnitude in units of the block's scale (at most 8, a float without error) and a draw of
-// 16 bits.  Above 1 the grid is that of a float with one bit of mantissa, so the code is the top of the float's own bits and the share of
-// the distance the 22 bits below; under 1 the spacing is 1/2 like that of the octave from 1 on, and 1 is added first, with what this
-// addition rounded away (`rest`) settling a tie.  Adding 2^22 - 33 - 64 u to the bits carries exactly where (u + 1/2) / 2^16 < share.
-__device__ inline uint32_t stochastic_code(float a, uint32_t u) {
-    const float one = a < 1.0f ? 1.0f : 0.0f;
-    const float t = a + one;
-    const uint32_t rest = a > t - one ? 1u : 0u;
-    const uint32_t v = (__float_as_uint(t) + (0x3FFFDFu - (u << 6)) + rest) >> 22;
-    return min(v - (a < 1.0f ? 254u : 252u), 7u);
+// One element, stochastically: its code, for a block whose scale has this inverse and a draw of 16 bits.  Its magnitude is scaled so that 1 in
+// units of the block becomes 2^-126: then the float's own bits are the grid, with its octaves of two steps each above 1 and, since floats
+// below 2^-126 are evenly spaced, the even steps of 1/2 below.  The code is the top of these bits and the share of the distance the 22 bits
+// below; adding 2^22 - 33 - 64 u to them carries exactly where (u + 1/2) / 2^16 < share.  What the scaling rounded down (`rest`) counts as
+// one more, since the border is a whole number: bits of the magnitude rounded up are above it exactly where the magnitude is.  (Products with
+// powers of two: an instruction that adds to the exponent takes four times as long.  The first one is exact but for magnitudes far below any
+// border.)
+__device__ inline uint32_t stochastic_code(float v, float inverse, uint32_t u) {
+    const float a = fabsf(v) * inverse, y = a * 0x1p-126f;
+    const uint32_t rest = y * 0x1p126f < a ? 1u : 0u;
+    return min((__float_as_uint(y) + (0x3FFFDFu - (u << 6)) + rest) >> 22, 7u);
 }
 
-// Eight elements into a word of codes; the block's scale byte comes back in s.  e: the octet's number, for the draws.
-template <bool SR> __device__ inline uint32_t encode8(const float* x, uint64_t e, uint32_t seed, uint32_t& s) {
+// The keys of a workgroup's draws: octet number `base` + o, 4 pairs of elements an octet; fewer than 2^30 octets lie in a workgroup, so that
+// the upper half of a pair's number takes two values at most.
+struct Draws {
+    uint64_t base;
+    uint32_t hi, key0, key1;
+    __device__ inline Draws(uint32_t seed, uint64_t first) : base(first), hi((uint32_t)(first >> 30)) {
+        key0 = fmix32(seed + 0x9E3779B9u * hi);
+        key1 = fmix32(seed + 0x9E3779B9u * (hi + 1u));
+    }
+    __device__ inline void of(uint32_t o, uint32_t (&h)[4]) const {
+        const uint64_t e = base + o;
+        const uint32_t key = (uint32_t)(e >> 30) == hi ? key0 : key1, lo = (uint32_t)e * 4u;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) h[i] = fmix32((lo + i) ^ key);
+    }
+};
+
+// Eight elements into a word of codes; the block's scale byte comes back in s.  o: the octet's number in the workgroup, for the draws.
+template <bool SR> __device__ inline uint32_t encode8(const float* x, const Draws& D, uint32_t o, uint32_t& s) {
     uint32_t peak = 0;
+#pragma unroll
     for (int i = 0; i < 8; i++) peak = max(peak, __float_as_uint(x[i]) & 0x7FFFFFFFu);
     peak = max_of_four(peak);
     const uint32_t ex = peak >> 23;
@@ -124,16 +146,13 @@ template <bool SR> __device__ inline uint32_t encode8(const float* x, uint64_t e
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], sc, 2);
         w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], sc, 3);
     } else {
-        const float inv = __uint_as_float((uint32_t)(254 - b) << 23);        // 2^(127 - b): exact, and so is the product with it
-        const uint64_t pair = e * 4;
-        const uint32_t key = sr_key(seed, pair);
-        for (int i = 0; i < 4; i++) {
-            const uint32_t h = fmix32(((uint32_t)pair + i) ^ key);
-            for (int j = 0; j < 2; j++) {
-                const float v = x[2 * i + j];
-                const uint32_t c = stochastic_code(fabsf(v) * inv, j ? h >> 16 : h & 0xFFFFu);
-                w |= (c | (__float_as_uint(v) >> 31) << 3) << (8 * i + 4 * j);
-            }
+        const float inverse = __uint_as_float((uint32_t)(254 - b) << 23);
+        uint32_t h[4];
+        D.of(o, h);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const uint32_t c = stochastic_code(x[i], inverse, i % 2 ? h[i / 2] >> 16 : h[i / 2] & 0xFFFFu);
+            w |= (c | (__float_as_uint(x[i]) >> 28 & 8u)) << (4 * i);
         }
     }
     s = bad ? 255u : (uint32_t)b;
@@ -159,10 +178,11 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(MxConvertArgs A) {
         p[u] = place(A.R, first + u * kThreads, limit);
         if (p[u].live) load8<T>(A.in, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, x[u]);
     }
+    const Draws D(A.seed, octets_before(A.R) + blockIdx.x * (kThreads * kOctets));
     for (uint32_t u = 0; u < kOctets; u++) {
         if (!p[u].live) continue;                     // (all four lanes of a block)
         uint32_t s;
-        const uint32_t w = encode8<SR>(x[u], (p[u].row * A.R.nb + p[u].blk) * 4 + p[u].q, A.seed, s);
+        const uint32_t w = encode8<SR>(x[u], D, u * kThreads + threadIdx.x, s);
         const uint64_t at = p[u].row * A.pitch + p[u].blk;
         *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p[u].q * 4) = w;
         if (p[u].q == 0) A.scales[at] = (uint8_t)s;
@@ -237,6 +257,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_sum(MxSumArgs<MAX> A) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     } else {
+        const Draws D(A.seed, octets_before(A.R) + blockIdx.x * (kThreads * U));
 #pragma unroll
         for (uint32_t u = 0; u < U; u++) {
             if (!p[u].live) continue;
@@ -247,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_sum(MxSumArgs<MAX> A) {
                 store_words<OUT, 8>(A.out, p[u].row, A.ld, p[u].blk * 32ull + p[u].q * 8u, A.R.cols, v);
             } else {
                 uint32_t s;
-                const uint32_t w = encode8<SR>(acc[u], (p[u].row * A.R.nb + p[u].blk) * 4 + p[u].q, A.seed, s);
+                const uint32_t w = encode8<SR>(acc[u], D, u * kThreads + threadIdx.x, s);
                 const uint64_t at = p[u].row * A.pitch + p[u].blk;
                 *reinterpret_cast<uint32_t*>(A.codes + at * 16 + p[u].q * 4) = w;
                 if (p[u].q == 0) A.scales[at] = (uint8_t)s;
