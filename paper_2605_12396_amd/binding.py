@@ -271,7 +271,9 @@ class Mx4:
                 or not scales.is_contiguous()):
             raise ValueError("codes [rows, 16 * pitch] and scales [rows, pitch] of uint8 are needed, contiguous")
         self.codes, self.scales, self.rows = codes, scales, scales.shape[0]
+        self.device = codes.get_device() if codes.device == scales.device else -1          # -1 (host memory too): refused by the calls
         self.c = Mx4Matrix(codes.data_ptr(), scales.data_ptr(), scales.shape[1])
+        self.ref = C.byref(self.c)
 
     @classmethod
     def empty(cls, rows, cols, device="cuda:0"):
@@ -288,12 +290,12 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _here(stream, *tensors):
-    """Whether the tensors lie on the current device, and the stream belongs to it."""
-    if any(t is not None and not t.is_cuda for t in tensors):
-        return False
-    dev = torch.cuda.current_device()
-    return all(t is None or t.get_device() == dev for t in tensors) and (stream is None or stream.device_index == dev)
+def _on(device, stream):
+    """The stream of a call whose tensors lie on `device`, as a number; None where that, or the stream's, is not the current device."""
+    if device < 0 or device != torch.cuda.current_device() or (stream is not None and stream.device_index != device):
+        return None
+    # (the stream that torch.cuda.current_stream() names; making that object takes 2.7 us, most of a small call)
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
 
 
 def nz_mx4_pitch(cols):
@@ -303,39 +305,41 @@ def nz_mx4_pitch(cols):
 def nz_mx4_quantize(d_in, rows, cols, ld, rounding, seed, out, stream=None):
     """d_in: float32, bfloat16 or float16 cuda tensor, ld elements from row to row; out: Mx4.  As every call on an Mx4 below:
     ERR_INVALID for tensors that do not lie on the current device, and for an Mx4 of fewer rows than the call names."""
-    if out.rows < rows or not _here(stream, d_in, out.codes, out.scales):
+    st = _on(out.device, stream)
+    if st is None or out.rows < rows or d_in.get_device() != out.device:
         return ERR_INVALID
-    return int(lib().nz_mx4_quantize(d_in.data_ptr(), _float_type(d_in), rows, cols, ld, rounding, seed, out.c, _stream(stream)))
+    return lib().nz_mx4_quantize(d_in.data_ptr(), _float_type(d_in), rows, cols, ld, rounding, seed, out.ref, st)
 
 
 def nz_mx4_dequantize(m, rows, cols, d_out, ld, stream=None):
-    if m.rows < rows or not _here(stream, m.codes, m.scales, d_out):
+    st = _on(m.device, stream)
+    if st is None or m.rows < rows or d_out.get_device() != m.device:
         return ERR_INVALID
-    return int(lib().nz_mx4_dequantize(m.c, rows, cols, d_out.data_ptr(), _float_type(d_out), ld, _stream(stream)))
+    return lib().nz_mx4_dequantize(m.ref, rows, cols, d_out.data_ptr(), _float_type(d_out), ld, st)
 
 
-def _mx4_operands(ms, rows, d_local, stream, *out):
+def _mx4_operands(ms, rows, d_local, device):
     """The host array of a sum's operands, or None where they do not fit."""
-    if any(m.rows < rows for m in ms) or not _here(stream, d_local, *out, *[t for m in ms for t in (m.codes, m.scales)]) or (
-            d_local is not None and d_local.dtype != torch.float32):
+    if any(m.rows < rows or m.device != device for m in ms):
+        return None
+    if d_local is not None and (d_local.dtype != torch.float32 or d_local.get_device() != device):
         return None
     return (Mx4Matrix * max(len(ms), 1))(*[m.c for m in ms])
 
 
 def nz_mx4_reduce_k(ms, d_local, ld_local, rows, cols, rounding, seed, out, stream=None):
     """ms: sequence of Mx4 (the host array is built here); d_local: float32 cuda tensor or None."""
-    ops = _mx4_operands(ms, rows, d_local, stream, out.codes, out.scales)
-    if ops is None or out.rows < rows:
+    st, ops = _on(out.device, stream), _mx4_operands(ms, rows, d_local, out.device)
+    if st is None or ops is None or out.rows < rows:
         return ERR_INVALID
-    return int(lib().nz_mx4_reduce_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, rounding, seed, out.c, _stream(stream)))
+    return lib().nz_mx4_reduce_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, rounding, seed, out.ref, st)
 
 
 def nz_mx4_sum_k(ms, d_local, ld_local, rows, cols, d_out, ld, stream=None):
-    ops = _mx4_operands(ms, rows, d_local, stream, d_out)
-    if ops is None:
+    st, ops = _on(d_out.get_device(), stream), _mx4_operands(ms, rows, d_local, d_out.get_device())
+    if st is None or ops is None:
         return ERR_INVALID
-    return int(lib().nz_mx4_sum_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, d_out.data_ptr(), _float_type(d_out), ld,
-                                  _stream(stream)))
+    return lib().nz_mx4_sum_k(ops, len(ms), _ptr(d_local), ld_local, rows, cols, d_out.data_ptr(), _float_type(d_out), ld, st)
 
 
 def nz_mx4_workspace_bytes(kind, left, m, n, k):
@@ -346,24 +350,32 @@ def nz_mx4_workspace_bytes(kind, left, m, n, k):
     return w
 
 
+def _mx4_workspace(d_ws, device):
+    return d_ws is None or d_ws.get_device() == device
+
+
 def nz_mx4_product(a, b, m, n, k, d_c, ldc, d_ws=None, ws_bytes=0, stream=None):
-    if a.rows < m or b.rows < n or not _here(stream, a.codes, a.scales, b.codes, b.scales, d_c, d_ws):
+    st = _on(b.device, stream)
+    if (st is None or a.rows < m or b.rows < n or a.device != b.device or d_c.get_device() != b.device
+            or not _mx4_workspace(d_ws, b.device)):
         return ERR_INVALID
-    return int(lib().nz_mx4_product(a.c, b.c, m, n, k, d_c.data_ptr(), _float_type(d_c), ldc, _ptr(d_ws), ws_bytes, _stream(stream)))
+    return lib().nz_mx4_product(a.ref, b.ref, m, n, k, d_c.data_ptr(), _float_type(d_c), ldc, _ptr(d_ws), ws_bytes, st)
+
+
+def _mx4_with_floats(fn, d_x, ldx, b, m, n, k, d_y, ldy, d_ws, ws_bytes, stream):
+    st = _on(b.device, stream)
+    if (st is None or b.rows < n or d_x.get_device() != b.device or d_y.get_device() != b.device
+            or not _mx4_workspace(d_ws, b.device)):
+        return ERR_INVALID
+    return fn(d_x.data_ptr(), _float_type(d_x), ldx, b.ref, m, n, k, d_y.data_ptr(), _float_type(d_y), ldy, _ptr(d_ws), ws_bytes, st)
 
 
 def nz_mx4_linear(d_x, ldx, b, m, n, k, d_c, ldc, d_ws=None, ws_bytes=0, stream=None):
-    if b.rows < n or not _here(stream, d_x, b.codes, b.scales, d_c, d_ws):
-        return ERR_INVALID
-    return int(lib().nz_mx4_linear(d_x.data_ptr(), _float_type(d_x), ldx, b.c, m, n, k, d_c.data_ptr(), _float_type(d_c), ldc,
-                                   _ptr(d_ws), ws_bytes, _stream(stream)))
+    return _mx4_with_floats(lib().nz_mx4_linear, d_x, ldx, b, m, n, k, d_c, ldc, d_ws, ws_bytes, stream)
 
 
 def nz_mx4_grad(d_g, ldg, b, m, n, k, d_da, ldda, d_ws=None, ws_bytes=0, stream=None):
-    if b.rows < n or not _here(stream, d_g, b.codes, b.scales, d_da, d_ws):
-        return ERR_INVALID
-    return int(lib().nz_mx4_grad(d_g.data_ptr(), _float_type(d_g), ldg, b.c, m, n, k, d_da.data_ptr(), _float_type(d_da), ldda,
-                                 _ptr(d_ws), ws_bytes, _stream(stream)))
+    return _mx4_with_floats(lib().nz_mx4_grad, d_g, ldg, b, m, n, k, d_da, ldda, d_ws, ws_bytes, stream)
 
 
 def read_result(d_res):
