@@ -99,9 +99,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     uint32_t part, first, steps;                                       // this workgroup's steps: from `first` to below `steps`
     uint32_t lo[LL], ro[RL ? RL : 1], slo[SL ? SL : 1], sro[SR ? SR : 1];
     uint32_t lchunk;
-    uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1, columns PW gq .. of a piece
-    i32x4 gw[2];
-    uint32_t gs[2];
+    uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1 and columns PW gq .. of a piece
 
     __device__ __forceinline__ explicit Tile(const TileArgs& args) : A(args) {
         uint32_t tm, tj;
@@ -149,21 +147,29 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         const bool in = OP == PRODUCT ? on & (s * 8 + lchunk < nb) : on & ((A.terms > 1) | ((uint64_t)rs * 64 + lchunk * 8 < A.inner));
 #pragma unroll
         for (int i = 0; i < LL; i++) load_lds<16>(bl, h->l + (i * NT + wave * 64) * 16, in ? lo[i] : kNowhere);
-        if (OP == GRAD) {
-            // (a piece of 32 columns is one block; one of 16 half of one)
+    }
+
+    // grad: a piece of the right for step s, to registers (a piece of 32 columns is one block; one of 16 half of one).
+    struct Piece { uint32_t w[2][PW / 8], s[2]; };
+    __device__ __forceinline__ void fetch_piece(uint32_t s, Piece& P) {
+        if constexpr (OP == GRAD) {
+            const uint32_t rs = right_step(s);
             const rsrc_t br = buffer_at(right + (uint64_t)rs * 64 * A.right_pitch), bs = buffer_at(right_s + (uint64_t)rs * 64 * A.right_spitch);
-            const bool c_in = gq * PW < (uint32_t)((A.outer + 31) / 32 * 32 - j0);
+            const bool c_in = (s < steps) & (gq * PW < (uint32_t)((A.outer + 31) / 32 * 32 - j0));
 #pragma unroll
             for (int r = 0; r < 2; r++) {
                 const uint32_t row = gd * 2 + r;
-                const bool in = on & c_in & ((uint64_t)rs * 64 + row < A.inner);
+                const bool in = c_in & ((uint64_t)rs * 64 + row < A.inner);
                 const uint32_t off = in ? row * (uint32_t)A.right_pitch + gq * (PW / 2) : kNowhere;
-                if constexpr (PW == 32) gw[r] = load16(br, off);
-                else {
+                if constexpr (PW == 32) {
+                    const i32x4 v = load16(br, off);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) P.w[r][i] = v[i];
+                } else {
                     const auto v = __builtin_amdgcn_raw_buffer_load_b64(br, off, 0, 0);
-                    gw[r][0] = v[0]; gw[r][1] = v[1];
+                    P.w[r][0] = v[0]; P.w[r][1] = v[1];
                 }
-                gs[r] = __builtin_amdgcn_raw_buffer_load_b8(bs, in ? row * (uint32_t)A.right_spitch + gq * PW / 32 : kNowhere, 0, 0);
+                P.s[r] = __builtin_amdgcn_raw_buffer_load_b8(bs, in ? row * (uint32_t)A.right_spitch + gq * PW / 32 : kNowhere, 0, 0);
             }
         }
     }
@@ -193,14 +199,14 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // grad: two rows of codes become columns of bf16, two rows to a word.
-    __device__ __forceinline__ void turn(Half* __restrict h) {
+    __device__ __forceinline__ void turn(const Piece& P, Half* __restrict h) {
         if constexpr (OP == GRAD) {
-            const float s0 = mx_scale(gs[0]), s1 = mx_scale(gs[1]);
+            const float s0 = mx_scale(P.s[0]), s1 = mx_scale(P.s[1]);
 #pragma unroll
             for (uint32_t w = 0; w < PW / 8; w++)
                 unroll4([&](auto B) {
-                    const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[0][w], s0, B.value));
-                    const uint32_t q = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(gw[1][w], s1, B.value));
+                    const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(P.w[0][w], s0, B.value));
+                    const uint32_t q = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(P.w[1][w], s1, B.value));
                     const uint32_t col = gq * PW + w * 8 + B.value * 2;
                     *reinterpret_cast<uint32_t*>(h->r + col * 128 + ((gd / 4 ^ col / 2 % 8) * 16) + gd % 4 * 4) = __builtin_amdgcn_perm(q, p, 0x05040100u);
                     *reinterpret_cast<uint32_t*>(h->r + (col + 1) * 128 + ((gd / 4 ^ col / 2 % 8) * 16) + gd % 4 * 4) =
@@ -297,8 +303,9 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // Step s, whose first fragments are in registers already.  The workgroup meets while the last of its four multiplications is still to
-    // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.
-    __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
+    // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.  (grad: P holds step s + 1
+    // of the right, and then gets step s + 3.)
+    __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Piece& P, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
         Frag F1, F2, F3;
         load_frag(1, cur, F1);
         widen<1>(S, F1);
@@ -311,10 +318,11 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         order<kGap, 0>();
         load_frag(3, cur, F3);
         widen<3>(S, F3);
-        turn(next);
+        turn(P, next);
         multiply<2>(F2, S, acc);
         order<kGap, 0, true>();
         meet();
+        fetch_piece(s + 3, P);
         fetch(s + 2, cur);
         Side S1;
         load_side(s + 1, next, S1);
@@ -389,10 +397,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
 #pragma unroll
         for (int b = 0; b < Tl::TN; b++) acc[a][b] = f32x16{};
     uint32_t s = T.first;
+    typename Tl::Piece P0, P1;                                         // of even and odd steps from the first, two steps ahead of their use
+    T.fetch_piece(s, P0);
+    T.fetch_piece(s + 1, P1);
     T.fetch(s, &h0);
     T.fetch_rest(s, &h0);
-    T.turn(&h0);
     T.fetch(s + 1, &h1);
+    T.turn(P0, &h0);
+    T.fetch_piece(s + 2, P0);
     T.meet();
     typename Tl::Frag F;
     typename Tl::Side S;
@@ -400,10 +412,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     T.load_frag(0, &h0, F);
     T.template widen<0>(S, F);
     for (; s + 1 < T.steps; s += 2) {
-        T.step(s, &h0, &h1, F, S, acc);
-        T.step(s + 1, &h1, &h0, F, S, acc);
+        T.step(s, &h0, &h1, P1, F, S, acc);
+        T.step(s + 1, &h1, &h0, P0, F, S, acc);
     }
-    if (s < T.steps) T.step(s, &h0, &h1, F, S, acc);
+    if (s < T.steps) T.step(s, &h0, &h1, P1, F, S, acc);
     Tl::meet();                                                        // (nor may a load reach shared memory after the workgroup's end)
     uint8_t* const scratch = reinterpret_cast<uint8_t*>(&h0);
     if (A.parts > 1) T.template store<float>(A.sums + T.part * A.M * A.sum_pitch, A.sum_pitch, scratch, acc);
