@@ -3,6 +3,7 @@
 // All three are C[m][j] = sum over i of left[m][i] * right[j][i]; in the gradient right is B seen by its columns, right[j][i] = B[i][j].
 // `inner` is the length of the sum, `outer` the number of columns of C.
 #include "nz_mx4.hpp"
+#include <algorithm>
 #include <type_traits>
 
 namespace nz {
@@ -738,17 +739,120 @@ template <int LEFT> hipError_t launch_rows(const RowArgs& R, hipStream_t st) {
     return hipGetLastError();
 }
 
+// The gradient for few rows: bound by the codes as well.  A workgroup of 8 waves takes 256 columns of B over a part of its rows; a wave takes
+// 32 rows at a time, a lane 8 of them (group g = lane / 16) in 16 columns (lane % 16), turns its 8 x 16 codes into 16 fragments of 8 rows in
+// registers, and multiplies them with the same 8 elements of up to 16 rows of the left: the j-th instruction makes the columns 16 i + j.
+// Columns need as many fragments as there are, so that nothing is exchanged between lanes.  The next 32 rows are on their way meanwhile.
+// Waves are added in their order through shared memory, parts by k_mx_join.  LEFT: as for k_mx_rows, floats.
+template <int LEFT>
+__global__ __launch_bounds__(512, 2) void k_mx_grad_rows(RowArgs A, uint32_t parts, float* sums, uint64_t sum_pitch) {
+    constexpr int terms = terms_of(LEFT);
+    struct Own { uint32_t scales[64]; };
+    union Shared { Own own[8]; float part[8][16][256]; };
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const uint32_t t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), c16 = lane % 16, g = lane / 16;
+    const uint32_t strips = gridDim.x / parts, strip = blockIdx.x % strips, part = blockIdx.x / strips;
+    const uint64_t j0 = (uint64_t)strip * 256;
+    const uint32_t cols = (uint32_t)min(A.outer - j0, (uint64_t)256), blocks = (cols + 31) / 32;
+    const uint32_t units = (uint32_t)((A.inner + 31) / 32), slices = parts * 8, slice = part * 8 + wave;
+    const uint32_t u0 = (uint32_t)((uint64_t)units * slice / slices), u1 = (uint32_t)((uint64_t)units * (slice + 1) / slices);
+    const uint32_t lo = min(c16, A.M - 1) * (uint32_t)A.left_pitch;
+    Own& own = sh.own[wave];
+
+    f32x4 acc[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) acc[i] = f32x4{};
+    uint2 w[8];
+    uint32_t sw;
+    Eight<LEFT> e;
+    auto ask = [&](uint32_t u) {
+        const uint64_t n0 = (uint64_t)u * 32;
+        const rsrc_t br = buffer_at(A.right + n0 * A.right_pitch + j0 / 2), bs = buffer_at(A.right_scales + n0 * A.right_spitch + j0 / 32);
+        const uint32_t here = u < u1 ? (uint32_t)min(A.inner - n0, (uint64_t)32) : 0;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; r++) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(br, ((g * 8 + r < here) & (c16 / 2 < blocks)) ? (g * 8 + r) * (uint32_t)A.right_pitch + c16 * 8 : kNowhere, 0, 0);
+            w[r] = make_uint2(v[0], v[1]);
+        }
+        // (a word holds the scales of four blocks of a row; those past the last block belong to columns that are not stored)
+        const uint32_t row = lane / 2;
+        sw = __builtin_amdgcn_raw_buffer_load_b32(bs, ((row < here) & (lane % 2 * 4 < blocks)) ? row * (uint32_t)A.right_spitch + lane % 2 * 4 : kNowhere, 0, 0);
+        e.load_words(buffer_at(A.left + n0 * float_bytes(LEFT)), g * 8 < here ? lo + g * 8 * float_bytes(LEFT) : kNowhere);
+    };
+    ask(u0);
+    for (uint32_t u = u0; u < u1; u++) {
+        own.scales[lane] = sw;
+        i32x4 x[terms];
+        e.terms(x);
+        uint2 now[8];
+#pragma unroll
+        for (int r = 0; r < 8; r++) now[r] = w[r];
+        ask(u + 1);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float sc[8];
+#pragma unroll
+        for (uint32_t r = 0; r < 8; r++) sc[r] = mx_scale(reinterpret_cast<const uint8_t*>(own.scales)[(g * 8 + r) * 8 + c16 / 2]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            unroll4([&](auto B) {
+                uint32_t p[8];
+#pragma unroll
+                for (int r = 0; r < 8; r++) p[r] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(h ? now[r].y : now[r].x, sc[r], B.value));
+                i32x4 even, odd;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    even[i] = (int)__builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x05040100u);
+                    odd[i] = (int)__builtin_amdgcn_perm(p[2 * i + 1], p[2 * i], 0x07060302u);
+                }
+                constexpr int j = B.value * 2;
+#pragma unroll
+                for (int q = 0; q < terms; q++) {
+                    acc[h * 8 + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[q]), __builtin_bit_cast(bf16x8, even), acc[h * 8 + j], 0, 0, 0);
+                    acc[h * 8 + j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[q]), __builtin_bit_cast(bf16x8, odd), acc[h * 8 + j + 1], 0, 0, 0);
+                }
+            });
+    }
+    __syncthreads();                                                    // (the sums take the place of the scales)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4)
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (g * 4 + i < A.M) {
+                const f32x4 v = { acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i] };
+                *reinterpret_cast<f32x4*>(&sh.part[wave][g * 4 + i][c16 * 16 + j]) = v;
+            }
+    __syncthreads();
+    for (uint32_t o = t; o < A.M * 256; o += 512) {
+        const uint32_t m = o / 256, j = o % 256;
+        if (j >= cols) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; k++) v += sh.part[k][m][j];
+        if (parts > 1) sums[((uint64_t)part * A.M + m) * sum_pitch + j0 + j] = v;
+        else store_one(A.c, A.c_type, m * A.ldc + j0 + j, v);
+    }
+}
+
 // Rows up to which k_mx_rows is taken.  Against 4096 x 4096 in four bits and with bf16, in microseconds: 32 rows 8.1 and 11.6, by tiles 13.3
 // and 16.4; 64 rows (with room for them in its registers) 11.8 and 19.1, by tiles 13.2 and 18.7, against 8192 x 8192 24.9 and 39.1, by
 // tiles 20.2 and 33.0.
 constexpr uint64_t kFewRows = 32;
+constexpr uint64_t kFewGradRows = 16;
 
 // Sums of the parts of a length, in their order, into C: a thread makes four neighbouring columns.
-__global__ __launch_bounds__(256) void k_mx_join(const float* sums, uint32_t parts, uint64_t M, uint64_t outer, uint64_t pitch, void* c, uint64_t ldc, int type) {
-    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x, per_row = pitch / 4, m = id / per_row, j = id % per_row * 4;
+__global__ __launch_bounds__(64) void k_mx_join(const float* sums, uint32_t parts, uint64_t M, uint64_t outer, uint64_t pitch, void* c, uint64_t ldc, int type) {
+    const uint64_t id = (uint64_t)blockIdx.x * 64 + threadIdx.x, per_row = pitch / 4, m = id / per_row, j = id % per_row * 4;
     if (m >= M) return;
     f32x4 v = {};
-    for (uint32_t p = 0; p < parts; p++) v += *reinterpret_cast<const f32x4*>(sums + (p * M + m) * pitch + j);
+    for (uint32_t p = 0; p < parts; p += 8) {                           // (eight on their way at once)
+        f32x4 w[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) w[i] = p + i < parts ? *reinterpret_cast<const f32x4*>(sums + ((p + i) * M + m) * pitch + j) : f32x4{};
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++)
+            if (p + i < parts) v += w[i];
+    }
     for (uint32_t i = 0; i < 4; i++)
         if (j + i < outer) store_one(c, type, m * ldc + j + i, v[i]);
 }
@@ -784,6 +888,11 @@ Plan plan_tiles(int op, uint64_t M, uint64_t outer, uint32_t steps) {
 
 uint64_t sum_pitch(uint64_t outer) { return (outer + 3) / 4 * 4; }
 
+void launch_join(const float* sums, uint32_t parts, uint64_t M, uint64_t outer, void* c, uint64_t ldc, int type, hipStream_t st) {
+    const uint64_t pitch = sum_pitch(outer);
+    hipLaunchKernelGGL(k_mx_join, dim3((uint32_t)((M * (pitch / 4) + 63) / 64)), dim3(64), 0, st, sums, parts, M, outer, pitch, c, ldc, type);
+}
+
 size_t sums_bytes(const Plan& p, uint64_t M, uint64_t outer) { return p.parts > 1 ? (size_t)p.parts * M * sum_pitch(outer) * 4 : 0; }
 
 template <int OP> hipError_t launch_tiles(TileArgs& T, const Plan& p, float* sums, hipStream_t st) {
@@ -792,9 +901,7 @@ template <int OP> hipError_t launch_tiles(TileArgs& T, const Plan& p, float* sum
     const dim3 grid(T.tiles_m * T.tiles_j * p.parts);
     if (p.tile == 256) hipLaunchKernelGGL((k_mx_tile<OP, 256, 256, 2, 2>), grid, dim3(256), 0, st, T);
     else hipLaunchKernelGGL((k_mx_tile<OP, 128, 128, 2, 2>), grid, dim3(256), 0, st, T);
-    if (p.parts > 1)
-        hipLaunchKernelGGL(k_mx_join, dim3((uint32_t)((T.M * (T.sum_pitch / 4) + 255) / 256)), dim3(256), 0, st, sums, p.parts, T.M, T.outer, T.sum_pitch,
-                           T.c, T.ldc, T.c_type);
+    if (p.parts > 1) launch_join(sums, p.parts, T.M, T.outer, T.c, T.ldc, T.c_type, st);
     return hipGetLastError();
 }
 
@@ -812,40 +919,71 @@ template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint3
                        A.ldx * float_bytes(T) % 16 == 0, A.M, inner, chunks, reinterpret_cast<uint16_t*>(A.ws));
 }
 
+size_t laid_bytes(int left, uint64_t M, uint64_t inner) { return (M * ((inner + 7) / 8 * 8) * float_bytes(left) + 255) / 256 * 256; }
+
+// Parts of the rows of B in k_mx_grad_rows: a workgroup for every compute unit, 32 rows at least for every wave; not more than one kernel
+// joins quickly.
+uint32_t grad_parts(uint64_t outer, uint64_t inner) {
+    const uint64_t strips = (outer + 255) / 256, most = (inner + 255) / 256;
+    const uint64_t parts = strips >= 256 ? 1 : 256 / strips;
+    return (uint32_t)std::min<uint64_t>(std::min(parts, most), 32);
+}
+
+// The left's floats for few rows: laid out anew where they cannot be read in 16-byte words.
+hipError_t lay_left(const MxProductArgs& A, int left, RowArgs& R, hipStream_t st) {
+    R.left = reinterpret_cast<const uint8_t*>(A.x); R.left_pitch = A.ldx * float_bytes(left);
+    if ((R.M == 1 || R.left_pitch % 16 == 0) && R.inner % 8 == 0) return hipSuccess;
+    const uint64_t row = (R.inner + 7) / 8 * 8 * float_bytes(left);
+    uint8_t* const ws = reinterpret_cast<uint8_t*>(A.ws);
+    const dim3 grid((uint32_t)((R.M * row / 16 + 255) / 256));
+    if (left == F32) hipLaunchKernelGGL((k_mx_lay<4>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
+    else hipLaunchKernelGGL((k_mx_lay<2>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
+    R.left = ws; R.left_pitch = row;
+    return hipGetLastError();
+}
+
+hipError_t launch_few(const MxProductArgs& A, int kind, int left, hipStream_t st) {
+    RowArgs R = {};
+    R.right = A.b.codes; R.right_pitch = A.b.pitch * 16; R.right_scales = A.b.scales; R.right_spitch = A.b.pitch;
+    R.M = (uint32_t)A.M; R.outer = kind == GRAD ? A.K : A.N; R.inner = kind == GRAD ? A.N : A.K;
+    R.c = A.c; R.ldc = A.ldc; R.c_type = A.c_type;
+    if (kind == PRODUCT) {
+        R.left = A.a.codes; R.left_pitch = A.a.pitch * 16; R.left_scales = A.a.scales; R.left_spitch = A.a.pitch;
+        return launch_rows<-1>(R, st);
+    }
+    const hipError_t e = lay_left(A, left, R, st);
+    if (e != hipSuccess) return e;
+    if (kind == LINEAR) {
+        R.inner = (R.inner + 7) / 8 * 8;                                // (laid out or not: the codes behind the end are 0)
+        return left == F32 ? launch_rows<F32>(R, st) : left == F16 ? launch_rows<F16>(R, st) : launch_rows<BF16>(R, st);
+    }
+    const uint32_t parts = grad_parts(R.outer, R.inner);
+    float* const sums = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(A.ws) + laid_bytes(left, A.M, R.inner));
+    const uint64_t pitch = sum_pitch(R.outer);
+    const dim3 grid((uint32_t)((R.outer + 255) / 256) * parts);
+    if (left == F32) hipLaunchKernelGGL((k_mx_grad_rows<F32>), grid, dim3(512), 0, st, R, parts, sums, pitch);
+    else if (left == F16) hipLaunchKernelGGL((k_mx_grad_rows<F16>), grid, dim3(512), 0, st, R, parts, sums, pitch);
+    else hipLaunchKernelGGL((k_mx_grad_rows<BF16>), grid, dim3(512), 0, st, R, parts, sums, pitch);
+    if (parts > 1) launch_join(sums, parts, R.M, R.outer, R.c, R.ldc, R.c_type, st);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t mx_product_workspace(int kind, int left, uint64_t M, uint64_t N, uint64_t K) {
     const uint64_t inner = kind == GRAD ? N : K, outer = kind == GRAD ? K : N;
-    if (kind != GRAD && M <= kFewRows) return kind == PRODUCT ? 0 : M * ((K + 7) / 8 * 8) * float_bytes(left);
+    if (kind != GRAD && M <= kFewRows) return kind == PRODUCT ? 0 : laid_bytes(left, M, inner);
+    if (kind == GRAD && M <= kFewGradRows) {
+        const uint32_t parts = grad_parts(outer, inner);
+        return laid_bytes(left, M, inner) + (parts > 1 ? parts * M * sum_pitch(outer) * 4 : 0);
+    }
     // (bf16 may need no terms, but then it has the plan of one term)
     const Plan p = plan_tiles(kind, M, outer, steps_of(kind, left, inner));
     return terms_bytes(kind, left, M, inner) + sums_bytes(p, M, outer);
 }
 
 hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStream_t st) {
-    if (kind != GRAD && A.M <= kFewRows) {
-        RowArgs R = {};
-        R.right = A.b.codes; R.right_pitch = A.b.pitch * 16; R.right_scales = A.b.scales; R.right_spitch = A.b.pitch;
-        R.M = (uint32_t)A.M; R.outer = A.N; R.inner = A.K;
-        R.c = A.c; R.ldc = A.ldc; R.c_type = A.c_type;
-        if (kind == PRODUCT) {
-            R.left = A.a.codes; R.left_pitch = A.a.pitch * 16; R.left_scales = A.a.scales; R.left_spitch = A.a.pitch;
-            return launch_rows<-1>(R, st);
-        }
-        R.left = reinterpret_cast<const uint8_t*>(A.x); R.left_pitch = A.ldx * float_bytes(left);
-        if ((A.M > 1 && R.left_pitch % 16) || A.K % 8) {
-            const uint64_t row = (A.K + 7) / 8 * 8 * float_bytes(left);
-            uint8_t* const ws = reinterpret_cast<uint8_t*>(A.ws);
-            const dim3 grid((uint32_t)((A.M * row / 16 + 255) / 256));
-            if (left == F32) hipLaunchKernelGGL((k_mx_lay<4>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
-            else hipLaunchKernelGGL((k_mx_lay<2>), grid, dim3(256), 0, st, R.left, R.left_pitch, R.M, R.inner, ws);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            R.left = ws; R.left_pitch = row;
-            R.inner = (A.K + 7) / 8 * 8;                          // (the codes there are 0)
-        }
-        return left == F32 ? launch_rows<F32>(R, st) : left == F16 ? launch_rows<F16>(R, st) : launch_rows<BF16>(R, st);
-    }
+    if (A.M <= (kind == GRAD ? kFewGradRows : kFewRows)) return launch_few(A, kind, left, st);
     TileArgs T = {};
     T.M = A.M; T.outer = kind == GRAD ? A.K : A.N; T.inner = kind == GRAD ? A.N : A.K;
     T.c = A.c; T.ldc = A.ldc; T.c_type = A.c_type;
