@@ -13,7 +13,8 @@ pytestmark = pytest.mark.gpu
 
 SIZES = [(1, 1, 1), (1, 17, 33), (1, 4096, 4096), (2, 64, 64), (3, 5, 7), (15, 100, 31), (16, 128, 128), (17, 33, 65), (31, 260, 520), (33, 128, 1000),
          (64, 64, 64), (65, 130, 257), (100, 96, 2050), (128, 256, 512), (129, 257, 513), (200, 1030, 96), (257, 300, 771), (300, 515, 4100),
-         (512, 512, 512), (520, 776, 1544), (48, 300, 7000), (150, 7000, 300), (31, 100, 6900), (260, 390, 6400), (1, 2, 5000), (5, 2500, 64), (1000, 40, 130), (1031, 1290, 320)]
+         (512, 512, 512), (520, 776, 1544), (48, 300, 7000), (150, 7000, 300), (31, 100, 6900), (260, 390, 6400), (1, 2, 5000), (5, 2500, 64), (1000, 40, 130), (1031, 1290, 320), (1, 8205, 260), (4, 9000, 2300),
+         (6, 8200, 1100), (20, 8200, 140)]
 
 
 def check(nz, kind, left, b, m, n, k, out, want, ld_pad=0, exact=True, slack=None):
@@ -80,6 +81,22 @@ def test_linear_and_grad_exact(nz, size, left):
         pad = (0, 8, 1)[i]                                               # rows of floats at 16 bytes or not, NaN behind them
         check(nz, nz.MX4_LINEAR, floats(nz, x, left, k + pad)[0], bm, m, n, k, out, x @ w.T, ld_pad=pad)
         check(nz, nz.MX4_GRAD, floats(nz, g, left, n + pad)[0], bm, m, n, k, out, g @ w, ld_pad=pad)
+
+
+@pytest.mark.parametrize("size", [(1, 40, 20000), (3, 40, 20000), (20, 24, 20011), (40, 24, 20000), (1, 20000, 300), (16, 20001, 40), (33, 20000, 264)],
+                         ids=str)
+def test_long_sums(nz, size):
+    """Scales of 1: multiples of 1/4 up to 36 and of 1/8 up to 12, so 36 * 20011 * 4 and 12 * 20011 * 8 are below 2^24."""
+    m, n, k = size
+    rng = np.random.default_rng(m + k)
+    a, b = R.random_matrix(rng, m, k, 127, 128), R.random_matrix(rng, n, k, 127, 128)
+    w = R.values(*b, k)
+    bm = mat(nz, *R.place(*b, k))
+    check(nz, nz.MX4_PRODUCT, mat(nz, *R.place(*a, k)), bm, m, n, k, "f32", R.values(*a, k) @ w.T)
+    for left in ("bf16", "f16", "f32"):
+        x, g = exact_floats(rng, m, k), exact_floats(rng, m, n)
+        check(nz, nz.MX4_LINEAR, floats(nz, x, left)[0], bm, m, n, k, "f32", x @ w.T)
+        check(nz, nz.MX4_GRAD, floats(nz, g, left)[0], bm, m, n, k, "f32", g @ w)
 
 
 @pytest.mark.parametrize("size", [(3588, 3850, 300), (3841, 4100, 1056)], ids=str)
