@@ -46,8 +46,8 @@ struct MxProductArgs {
 };
 
 hipError_t launch_mx_quantize(const MxConvertArgs& A, int type, bool stochastic, hipStream_t st);
-// type: of the floats that are written, or -1 for four bits
-template <uint32_t MAX> hipError_t launch_mx_sum(const MxSumArgs<MAX>& A, int type, bool stochastic, hipStream_t st);
+// type: of the floats that are written, or -1 for four bits; way: four bits stochastically, floats around the caches
+template <uint32_t MAX> hipError_t launch_mx_sum(const MxSumArgs<MAX>& A, int type, bool way, hipStream_t st);
 
 size_t mx_product_workspace(int kind, int left, uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_mx_product(const MxProductArgs& A, int kind, int left, hipStream_t st);

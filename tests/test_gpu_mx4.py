@@ -245,6 +245,22 @@ def test_capture_and_streams(nz):
         assert torch.equal(got, eager) and got.abs().sum() > 0
 
 
+@pytest.mark.parametrize("name", ["f32", "f16"])
+def test_large_floats_equal_small_ones(nz, name):
+    """Floats of more than 128 MB take another way to memory; the same rows, one call each, do not."""
+    import torch
+    rows, cols, ld = 3, 23000001 if name == "f16" else 12000001, 23000004
+    m = nz.Mx4.empty(rows, cols)
+    m.codes.random_(0, 256)
+    m.scales.random_(110, 140)
+    whole, single = (torch.full((rows, ld), 3.0, dtype=dtype(name), device="cuda:0") for _ in range(2))
+    assert nz.nz_mx4_sum_k([m, m], None, 0, rows, cols, whole, ld) == 0
+    for r in range(rows):
+        one = nz.Mx4(m.codes[r:r + 1], m.scales[r:r + 1])
+        assert nz.nz_mx4_sum_k([one, one], None, 0, 1, cols, single[r], ld) == 0
+    assert torch.equal(whole, single) and (whole[:, cols:] == 3).all() and whole[:, :cols].abs().max() > 4
+
+
 def test_offsets_past_32_bits(nz):
     """9.2e9 elements: 18 GB of bf16 and 4.9 GB of codes, whole rows and ragged ones; rows at both ends and around 2^32 bytes are looked at."""
     import torch
