@@ -249,10 +249,10 @@ def test_capture_and_streams(nz):
 def test_large_floats_equal_small_ones(nz, name):
     """Floats of more than 128 MB take another way to memory; the same rows, one call each, do not."""
     import torch
-    rows, cols, ld = 3, 23000001 if name == "f16" else 12000001, 23000004
-    m = nz.Mx4.empty(rows, cols)
-    m.codes.random_(0, 256)
-    m.scales.random_(110, 140)
+    rows, cols, ld = 3, 23000001 if name == "f16" else 12000001, 23000008
+    pitch = 718752                                                       # (rows of scales, and of floats, at multiples of 16 bytes)
+    m = nz.Mx4(torch.randint(0, 256, (rows, 16 * pitch), dtype=torch.uint8, device="cuda:0"),
+               torch.randint(110, 140, (rows, pitch), dtype=torch.uint8, device="cuda:0"))
     whole, single = (torch.full((rows, ld), 3.0, dtype=dtype(name), device="cuda:0") for _ in range(2))
     assert nz.nz_mx4_sum_k([m, m], None, 0, rows, cols, whole, ld) == 0
     for r in range(rows):
