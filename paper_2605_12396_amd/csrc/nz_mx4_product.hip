@@ -487,7 +487,7 @@ template <int T>
 __global__ __launch_bounds__(256) void k_mx_terms(const uint8_t* x, uint64_t ldx, bool wide, uint64_t M, uint64_t inner, uint32_t chunks,
                                                   uint16_t* out) {
     constexpr int terms = terms_of(T);
-    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;               // 8 elements
+    const uint64_t id = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;       // 8 elements
     const uint64_t per_row = (uint64_t)chunks * 8;
     const uint64_t m = id / per_row;
     if (m >= M) return;
@@ -917,7 +917,8 @@ uint32_t steps_of(int kind, int left, uint64_t inner) {
 size_t terms_bytes(int kind, int left, uint64_t M, uint64_t inner) { return kind == PRODUCT ? 0 : (inner + 63) / 64 * 128 * M * terms_of(left); }
 
 template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint32_t chunks, hipStream_t st) {
-    hipLaunchKernelGGL((k_mx_terms<T>), dim3((uint32_t)((A.M * chunks * 8 + 255) / 256)), dim3(256), 0, st, reinterpret_cast<const uint8_t*>(A.x), A.ldx,
+    const uint64_t groups = (A.M * chunks * 8 + 255) / 256, x = std::min<uint64_t>(groups, 1u << 22);       // (a launch has fewer than 2^32 threads along x)
+    hipLaunchKernelGGL((k_mx_terms<T>), dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x)), dim3(256), 0, st, reinterpret_cast<const uint8_t*>(A.x), A.ldx,
                        A.ldx * float_bytes(T) % 16 == 0, A.M, inner, chunks, reinterpret_cast<uint16_t*>(A.ws));
 }
 

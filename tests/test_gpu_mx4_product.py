@@ -287,6 +287,26 @@ def test_codes_past_32_bits(nz):
         assert (y.cpu().numpy() == w[-1]).all()
 
 
+def test_a_very_tall_left_side(nz):
+    """More rows than one launch has threads for along x, where their floats are laid out anew (rows of two bytes): 69 GB of workspace."""
+    import torch
+    m = (1 << 29) + 5
+    b = nz.Mx4.empty(1, 1, "cuda:0")
+    b.codes.zero_()
+    b.codes[0, 0] = 5                                                    # 3
+    b.scales.fill_(128)                                                  # times 2
+    x = (torch.arange(m, device="cuda:0", dtype=torch.int32) % 251 - 100).bfloat16()
+    for call, kind in ((nz.nz_mx4_linear, nz.MX4_LINEAR), (nz.nz_mx4_grad, nz.MX4_GRAD)):
+        wsb = nz.nz_mx4_workspace_bytes(kind, x.dtype, m, 1, 1)
+        y, ws = torch.full((m + 8,), 9.0, dtype=torch.bfloat16, device="cuda:0"), torch.empty(wsb, dtype=torch.uint8, device="cuda:0")
+        assert call(x, 1, b, m, 1, 1, y, 1, ws, wsb) == 0
+        for at in range(0, m, 1 << 27):                                  # (6 times eight bits, rounded once)
+            assert torch.equal(y[at:min(at + (1 << 27), m)], (x[at:at + (1 << 27)].float() * 6).bfloat16())
+        assert (y[m:] == 9).all()
+        del y, ws
+    torch.cuda.empty_cache()
+
+
 def test_a_sharded_training_step(nz):
     """As it is used: each of four ranks sends its weight shard in four bits, the gathered weights are multiplied as they landed, the gradient
     goes back through them, and the ranks' weight gradients are rounded without bias, summed into the shard's floats, and handed on."""
