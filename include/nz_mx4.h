@@ -89,8 +89,10 @@ size_t nz_mx4_workspace_bytes(nz_mx4_kind kind, nz_float_type left, size_t M, si
 nz_status nz_mx4_product(const nz_mx4_matrix* a, const nz_mx4_matrix* b, size_t M, size_t N, size_t K, void* d_c,
                          nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream);
 
-/* The same with floats on the left: C = X B^T, X[m][k] = d_x[m * ldx + k] of type x_type.  X is not rounded.
- * (Elements of B past the range of float32, 4 and 6 times 2^127, are infinite here and in nz_mx4_grad, as in nz_mx4_dequantize.) */
+/* The same with floats on the left: C = X B^T, X[m][k] = d_x[m * ldx + k] of type x_type.  X is not rounded,
+ * but bits of a float32 below 2^-133 are cut off (it is multiplied in terms of bfloat16).  Elements of B past the range of float32, 4 and 6
+ * times 2^127, are infinite in nz_mx4_dequantize; here and in nz_mx4_grad their products are not finite (infinite, or NaN as those of an
+ * infinity and 0). */
 nz_status nz_mx4_linear(const void* d_x, nz_float_type x_type, size_t ldx, const nz_mx4_matrix* b, size_t M, size_t N, size_t K,
                         void* d_c, nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream);
 

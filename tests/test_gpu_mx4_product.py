@@ -206,6 +206,40 @@ def test_extreme_scales(nz):
         check(nz, nz.MX4_PRODUCT, mat(nz, *R.place(*a, k)), mat(nz, *R.place(*b, k)), m, n, k, "f32", R.values(*a, k) @ R.values(*b, k).T)
 
 
+@pytest.mark.parametrize("m", [1, 20, 40, 300])
+def test_small_floats(nz, m):
+    """Multiples of 2^-133 (floats without their leading bit) against large weights, 2^100 against the smallest weights, and results that
+    are small: no product or sum is flushed.  Multiples of a power of two as in the exact cases.  Bits of float32 below 2^-133 are cut off."""
+    n, k = 136, 264
+    rng = np.random.default_rng(m)
+    for e, s in ((-131, 240), (100, 0), (-60, 62), (-64, 62)):
+        b = R.random_matrix(rng, n, k, s, s + 3)
+        w = R.values(*b, k)
+        bm = mat(nz, *R.place(*b, k))
+        x, g = exact_floats(rng, m, k) * 2.0 ** e, exact_floats(rng, m, n) * 2.0 ** e
+        for left in ("bf16", "f32"):
+            low_x, low_g = (np.copysign(rng.integers(0, 2 ** 16, v.shape) * 2.0 ** -149, v) if left == "f32" and e == -131 else 0 for v in (x, g))
+            check(nz, nz.MX4_LINEAR, floats(nz, x + low_x, left)[0], bm, m, n, k, "f32", x @ w.T)
+            check(nz, nz.MX4_GRAD, floats(nz, g + low_g, left)[0], bm, m, n, k, "f32", g @ w)
+
+
+def test_weights_past_the_range_of_float32(nz):
+    n, k = 48, 64
+    b = nz.Mx4.empty(n, k, "cuda:0")
+    b.codes.fill_(0x66)                                                  # 4
+    b.scales.fill_(254)                                                  # times 2^127
+    import torch
+    for m in (1, 20, 40):
+        for left in ("bf16", "f16", "f32"):
+            for call, kind, inner, outer in ((nz.nz_mx4_linear, nz.MX4_LINEAR, k, n), (nz.nz_mx4_grad, nz.MX4_GRAD, n, k)):
+                x = torch.full((m, inner), 1.5, dtype=dtype(left), device="cuda:0")
+                y = torch.zeros(m, outer, device="cuda:0")
+                wsb = nz.nz_mx4_workspace_bytes(kind, x.dtype, m, n, k)
+                ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device="cuda:0")
+                assert call(x, inner, b, m, n, k, y, outer, ws, wsb) == 0
+                assert not y.isfinite().any()
+
+
 def test_grad_against_differences(nz):
     """C is linear in X, so a difference of C along any direction is the gradient's product with it, to the roundings of both."""
     import torch
