@@ -72,15 +72,18 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
     static constexpr uint32_t RB = OP == LINEAR ? 32 : 128;            // bytes of a row of the right in shared memory
     static constexpr int LL = BM * 8 / NT, RL = OP == GRAD ? 0 : BN * (RB / 16) / NT;      // 16-byte loads of a thread
-    static constexpr int SL = OP == PRODUCT ? BM * 2 / NT : 0;                             // 4-byte loads of scales
-    static constexpr int SR = OP == PRODUCT ? BN * 2 / NT : OP == LINEAR ? (BN + NT - 1) / NT : 0;
+    static constexpr int SL = OP == PRODUCT ? BM * 4 / NT : 0;                             // 4-byte loads of scales (product: of a pair of steps)
+    static constexpr int SR = OP == PRODUCT ? BN * 4 / NT : OP == LINEAR ? (BN + NT - 1) / NT : 0;
     static constexpr uint32_t PW = BN * 32 / NT;                       // grad: columns of a thread's piece, two rows deep
 
     struct Half {
         uint8_t l[BM * 128];
         uint8_t r[BN * RB];
-        uint8_t sl[OP == PRODUCT ? BM * 8 : 16];
-        uint8_t sr[OP == PRODUCT ? BN * 8 : OP == LINEAR ? BN * 4 : 16];
+        uint8_t sr[OP == LINEAR ? BN * 4 : 16];
+    };
+    // product: the scales of a pair of steps
+    struct Scales {
+        uint8_t l[OP == PRODUCT ? BM * 16 : 16], r[OP == PRODUCT ? BN * 16 : 16];
     };
 
     // Results leave through a half's memory: 32 rows of as many columns as it has room for from every wave.  Bytes of such a row, with 16
@@ -127,10 +130,10 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
             ro[i] = OP == PRODUCT ? min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16
                                   : min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_pitch + (t % 2 ^ t / 16 % 2) * 16;
 #pragma unroll
-        for (int i = 0; i < SL; i++) slo[i] = min(t / 2 + NT / 2 * i, rows - 1) * (uint32_t)A.left_spitch + t % 2 * 4;
+        for (int i = 0; i < SL; i++) slo[i] = min(t / 4 + NT / 4 * i, rows - 1) * (uint32_t)A.left_spitch + t % 4 * 4;
 #pragma unroll
         for (int i = 0; i < SR; i++)
-            sro[i] = OP == PRODUCT ? min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_spitch + t % 2 * 4
+            sro[i] = OP == PRODUCT ? min(t / 4 + NT / 4 * i, cols - 1) * (uint32_t)A.right_spitch + t % 4 * 4
                                    : min(t + NT * i, cols - 1) * (uint32_t)A.right_spitch;
         gd = t % 32; gq = t / 32;
     }
@@ -183,19 +186,23 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
             const bool r_in = OP == PRODUCT ? on & (s * 8 + lchunk < nb) : on & (rs * 2 + (t % 2 ^ t / 16 % 2) < nb);
 #pragma unroll
             for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, r_in ? ro[i] : kNowhere);
-            if (OP == PRODUCT) {
-                const rsrc_t bsl = buffer_at(left_s + (uint64_t)s * 8), bsr = buffer_at(right_s + (uint64_t)s * 8);
-                const bool s_in = on & (s * 8 + t % 2 * 4 < nb);
-#pragma unroll
-                for (int i = 0; i < SL; i++) load_lds<4>(bsl, h->sl + (i * NT + wave * 64) * 4, s_in ? slo[i] : kNowhere);
-#pragma unroll
-                for (int i = 0; i < SR; i++) load_lds<4>(bsr, h->sr + (i * NT + wave * 64) * 4, s_in ? sro[i] : kNowhere);
-            } else {
+            if constexpr (OP == LINEAR) {
                 const rsrc_t bsr = buffer_at(right_s + (uint64_t)(rs / 2) * 4);     // (the scales of two steps)
 #pragma unroll
                 for (int i = 0; i < SR; i++)
                     if (BN % NT == 0 || wave * 64 < BN) load_lds<4>(bsr, h->sr + (i * NT + wave * 64) * 4, on ? sro[i] : kNowhere);
             }
+        }
+    }
+
+    // product: the scales of steps s and s + 1, of one side.
+    template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Scales* __restrict h) {
+        if constexpr (OP == PRODUCT) {
+            const rsrc_t b = buffer_at((RIGHT ? right_s : left_s) + (uint64_t)s * 8);
+            const bool in = (s < steps) & (s * 8 + t % 4 * 4 < nb);
+#pragma unroll
+            for (int i = 0; i < (RIGHT ? SR : SL); i++)
+                load_lds<4>(b, (RIGHT ? h->r : h->l) + (i * NT + wave * 64) * 4, in ? (RIGHT ? sro : slo)[i] : kNowhere);
         }
     }
 
@@ -220,14 +227,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     struct Frag { i32x4 x[TM], y[TN]; };
     struct Side { int sl[TM], sr[TN]; i32x4 w[TN]; };
 
-    __device__ __forceinline__ void load_side(uint32_t s, const Half* __restrict h, Side& S) {
+    // SECOND: s is the second step of its pair
+    template <bool SECOND> __device__ __forceinline__ void load_side(uint32_t s, const Half* __restrict h, const Scales* __restrict sc, Side& S) {
         if constexpr (OP == PRODUCT) {
             const uint32_t in = nb - min(s * 8 + g * 4, nb);           // blocks of this lane's four that there are
             const int keep = in >= 4 ? -1 : (1 << 8 * in) - 1;
 #pragma unroll
-            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(h->sl + (wm + a * 32 + l32) * 8 + g * 4) & keep;
+            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(sc->l + (wm + a * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
 #pragma unroll
-            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(h->sr + (wj + b * 32 + l32) * 8 + g * 4) & keep;
+            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(sc->r + (wj + b * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
         }
         if constexpr (OP == LINEAR) {
             const uint32_t blk = right_step(s) * 2 + g;
@@ -305,12 +313,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 
     // Step s, whose first fragments are in registers already.  The workgroup meets while the last of its four multiplications is still to
     // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.  (grad: P holds step s + 1
-    // of the right, and then gets step s + 3.)
-    __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Piece& P, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
+    // of the right, and then gets step s + 3.  product: sc has the scales of this pair of steps, and sn is filled with the next one's, one side in
+    // either step.)
+    template <bool SECOND> __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Scales* __restrict sc, Scales* __restrict sn, Piece& P,
+                                                                Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
         Frag F1, F2, F3;
         load_frag(1, cur, F1);
         widen<1>(S, F1);
         fetch_rest(s + 1, next);
+        fetch_scales<SECOND>(SECOND ? s + 1 : s + 2, sn);
         multiply<0>(F, S, acc);
         order<kGap, 2>();
         load_frag(2, cur, F2);
@@ -326,7 +337,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         fetch_piece(s + 3, P);
         fetch(s + 2, cur);
         Side S1;
-        load_side(s + 1, next, S1);
+        load_side<!SECOND>(s + 1, next, SECOND ? sn : sc, S1);
         load_frag(0, next, F);
         widen<0>(S1, F);
         multiply<3>(F3, S, acc);
@@ -391,6 +402,8 @@ template <int OP, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     typedef Tile<OP, BM, BN, WM, WN> Tl;
     __shared__ __attribute__((aligned(16))) typename Tl::Half h0, h1;
+    __shared__ __attribute__((aligned(16))) typename Tl::Scales scales[2];
+    typename Tl::Scales *sc = scales, *sn = scales + 1;
     Tl T(A);
     f32x16 acc[Tl::TM][Tl::TN];
 #pragma unroll
@@ -403,20 +416,24 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     T.fetch_piece(s + 1, P1);
     T.fetch(s, &h0);
     T.fetch_rest(s, &h0);
+    T.template fetch_scales<false>(s, sc);
+    T.template fetch_scales<true>(s, sc);
     T.fetch(s + 1, &h1);
     T.turn(P0, &h0);
     T.fetch_piece(s + 2, P0);
     T.meet();
     typename Tl::Frag F;
     typename Tl::Side S;
-    T.load_side(s, &h0, S);
+    T.template load_side<false>(s, &h0, sc, S);
     T.load_frag(0, &h0, F);
     T.template widen<0>(S, F);
     for (; s + 1 < T.steps; s += 2) {
-        T.step(s, &h0, &h1, P1, F, S, acc);
-        T.step(s + 1, &h1, &h0, P0, F, S, acc);
+        T.template step<false>(s, &h0, &h1, sc, sn, P1, F, S, acc);
+        T.template step<true>(s + 1, &h1, &h0, sc, sn, P0, F, S, acc);
+        typename Tl::Scales* const was = sc;
+        sc = sn; sn = was;
     }
-    if (s < T.steps) T.step(s, &h0, &h1, P1, F, S, acc);
+    if (s < T.steps) T.template step<false>(s, &h0, &h1, sc, sn, P1, F, S, acc);
     Tl::meet();                                                        // (nor may a load reach shared memory after the workgroup's end)
     uint8_t* const scratch = reinterpret_cast<uint8_t*>(&h0);
     if (A.parts > 1) T.template store<float>(A.sums + T.part * A.M * A.sum_pitch, A.sum_pitch, scratch, acc);
