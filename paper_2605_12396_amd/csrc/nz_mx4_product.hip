@@ -70,21 +70,21 @@ __device__ inline void tile_of(const TileArgs& A, uint32_t& tm, uint32_t& tj) {
 template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     static constexpr uint32_t NT = 64 * WM * WN;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-    static constexpr uint32_t RB = OP == LINEAR ? 32 : 128;            // bytes of a row of the right in shared memory
-    static constexpr int LL = BM * 8 / NT, RL = OP == GRAD ? 0 : BN * (RB / 16) / NT;      // 16-byte loads of a thread
-    static constexpr int SL = OP == PRODUCT ? BM * 4 / NT : 0;                             // 4-byte loads of scales (product: of a pair of steps)
-    static constexpr int SR = OP == PRODUCT ? BN * 4 / NT : OP == LINEAR ? (BN + NT - 1) / NT : 0;
+    static constexpr int LL = BM * 8 / NT, RL = OP == PRODUCT ? BN * 8 / NT : 0;           // 16-byte loads of a thread
+    static constexpr int SL = OP == PRODUCT ? BM * 4 / NT : 0, SR = OP == PRODUCT ? BN * 4 / NT : 0;       // 4-byte loads of a pair's scales
     static constexpr uint32_t PW = BN * 32 / NT;                       // grad: columns of a thread's piece, two rows deep
 
     struct Half {
         uint8_t l[BM * 128];
-        uint8_t r[BN * RB];
-        uint8_t sr[OP == LINEAR ? BN * 4 : 16];
+        uint8_t r[OP == LINEAR ? BN * 32 : BN * 128];                   // (linear: room for results)
     };
-    // product: the scales of a pair of steps
-    struct Scales {
-        uint8_t l[OP == PRODUCT ? BM * 16 : 16], r[OP == PRODUCT ? BN * 16 : 16];
+    // What is loaded for several steps at a time, since a request to the L2 costs the same for 8 bytes of a row as for 128.  product: the scales
+    // of the left and of the right for a pair of steps; linear: the right's scales and codes for four steps of it, which are 128 bytes of a row.
+    // (8192^3 in four bits 281 us instead of 303; 4096 rows of bf16 through 4096 x 8192 202 instead of 214, 512 through 8192 x 8192 81 instead of 98.)
+    struct Group {
+        uint8_t s[OP == PRODUCT ? BM * 16 : OP == LINEAR ? BN * 8 : 16], r[OP == PRODUCT ? BN * 16 : OP == LINEAR ? BN * 128 : 16];
     };
+    static_assert(OP != LINEAR || NT == BN * 2, "");
 
     // Results leave through a half's memory: 32 rows of as many columns as it has room for from every wave.  Bytes of such a row, with 16
     // more that spread the rows over the banks; columns in tiles of 32.
@@ -101,6 +101,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     uint64_t m0, j0;
     const uint8_t *left, *right, *left_s, *right_s;
     uint32_t part, first, steps;                                       // this workgroup's steps: from `first` to below `steps`
+    uint32_t right0;                                                   // linear: the right's first step, an even number
     uint32_t lo[LL], ro[RL ? RL : 1], slo[SL ? SL : 1], sro[SR ? SR : 1];
     uint32_t lchunk;
     uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1 and columns PW gq .. of a piece
@@ -111,8 +112,11 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         tm = __builtin_amdgcn_readfirstlane(tm); tj = __builtin_amdgcn_readfirstlane(tj);      // (the same in all lanes anyway)
         m0 = (uint64_t)tm * BM; j0 = (uint64_t)tj * BN;
         part = __builtin_amdgcn_readfirstlane(blockIdx.x / (A.tiles_m * A.tiles_j));
-        first = (uint32_t)((uint64_t)A.steps * part / A.parts); steps = (uint32_t)((uint64_t)A.steps * (part + 1) / A.parts);
+        const uint32_t unit = OP == LINEAR ? 2 * A.terms : 1, units = (A.steps + unit - 1) / unit;
+        first = min((uint32_t)((uint64_t)units * part / A.parts) * unit, A.steps);
+        steps = min((uint32_t)((uint64_t)units * (part + 1) / A.parts) * unit, A.steps);
         first = __builtin_amdgcn_readfirstlane(first); steps = __builtin_amdgcn_readfirstlane(steps);
+        right0 = __builtin_amdgcn_readfirstlane(right_step(first));
         t = threadIdx.x; lane = t % 64; wave = __builtin_amdgcn_readfirstlane(t / 64);
         g = lane / 32; l32 = lane % 32;
         wm = wave / WN * (BM / WM); wj = wave % WN * (BN / WN);
@@ -126,15 +130,11 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 #pragma unroll
         for (int i = 0; i < LL; i++) lo[i] = min(t / 8 + NT / 8 * i, rows - 1) * (uint32_t)A.left_pitch + lchunk * 16;
 #pragma unroll
-        for (int i = 0; i < RL; i++)
-            ro[i] = OP == PRODUCT ? min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16
-                                  : min(t / 2 + NT / 2 * i, cols - 1) * (uint32_t)A.right_pitch + (t % 2 ^ t / 16 % 2) * 16;
+        for (int i = 0; i < RL; i++) ro[i] = min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16;
 #pragma unroll
         for (int i = 0; i < SL; i++) slo[i] = min(t / 4 + NT / 4 * i, rows - 1) * (uint32_t)A.left_spitch + t % 4 * 4;
 #pragma unroll
-        for (int i = 0; i < SR; i++)
-            sro[i] = OP == PRODUCT ? min(t / 4 + NT / 4 * i, cols - 1) * (uint32_t)A.right_spitch + t % 4 * 4
-                                   : min(t + NT * i, cols - 1) * (uint32_t)A.right_spitch;
+        for (int i = 0; i < SR; i++) sro[i] = min(t / 4 + NT / 4 * i, cols - 1) * (uint32_t)A.right_spitch + t % 4 * 4;
         gd = t % 32; gq = t / 32;
     }
 
@@ -178,31 +178,48 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         }
     }
 
-    __device__ __forceinline__ void fetch_rest(uint32_t s, Half* __restrict h) {
-        if constexpr (OP != GRAD) {
-            const uint32_t rs = right_step(s);
-            const bool on = s < steps;
-            const rsrc_t br = buffer_at(right + (uint64_t)rs * RB);
-            const bool r_in = OP == PRODUCT ? on & (s * 8 + lchunk < nb) : on & (rs * 2 + (t % 2 ^ t / 16 % 2) < nb);
+    // product: the right for step s.
+    __device__ __forceinline__ void fetch_right(uint32_t s, Half* __restrict h) {
+        if constexpr (OP == PRODUCT) {
+            const rsrc_t br = buffer_at(right + (uint64_t)s * 128);
+            const bool in = (s < steps) & (s * 8 + lchunk < nb);
 #pragma unroll
-            for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, r_in ? ro[i] : kNowhere);
-            if constexpr (OP == LINEAR) {
-                const rsrc_t bsr = buffer_at(right_s + (uint64_t)(rs / 2) * 4);     // (the scales of two steps)
-#pragma unroll
-                for (int i = 0; i < SR; i++)
-                    if (BN % NT == 0 || wave * 64 < BN) load_lds<4>(bsr, h->sr + (i * NT + wave * 64) * 4, on ? sro[i] : kNowhere);
-            }
+            for (int i = 0; i < RL; i++) load_lds<16>(br, h->r + (i * NT + wave * 64) * 16, in ? ro[i] : kNowhere);
         }
     }
 
-    // product: the scales of steps s and s + 1, of one side.
-    template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Scales* __restrict h) {
-        if constexpr (OP == PRODUCT) {
-            const rsrc_t b = buffer_at((RIGHT ? right_s : left_s) + (uint64_t)s * 8);
-            const bool in = (s < steps) & (s * 8 + t % 4 * 4 < nb);
+    // The group that step s belongs to, counted from the first.
+    __device__ __forceinline__ uint32_t group_of(uint32_t s) const {
+        return OP == PRODUCT ? (s - first) / 2 : OP == LINEAR ? (right_step(s) - right0) / 4 : 0;
+    }
+
+    // A share of a group.  product: the scales of one side for steps s and s + 1.  linear: quarter q of the rows, from step rs of the right on.
+    template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Group* __restrict to) {
+        const rsrc_t b = buffer_at((RIGHT ? right_s : left_s) + (uint64_t)s * 8);
+        const bool in = (s < steps) & (s * 8 + t % 4 * 4 < nb);
 #pragma unroll
-            for (int i = 0; i < (RIGHT ? SR : SL); i++)
-                load_lds<4>(b, (RIGHT ? h->r : h->l) + (i * NT + wave * 64) * 4, in ? (RIGHT ? sro : slo)[i] : kNowhere);
+        for (int i = 0; i < (RIGHT ? SR : SL); i++)
+            load_lds<4>(b, (RIGHT ? to->r : to->s) + (i * NT + wave * 64) * 4, in ? (RIGHT ? sro : slo)[i] : kNowhere);
+    }
+    __device__ __forceinline__ void fetch_quarter(uint32_t rs, uint32_t q, Group* __restrict to) {
+        const rsrc_t br = buffer_at(right + (uint64_t)rs * 32), bs = buffer_at(right_s + (uint64_t)rs * 2);
+        const uint32_t row = min(t / 8 + NT / 8 * q, cols - 1);
+        load_lds<16>(br, to->r + (q * NT + wave * 64) * 16, rs * 2 + lchunk < nb ? row * (uint32_t)A.right_pitch + lchunk * 16 : kNowhere);
+        if (wave % 4 == q)
+            load_lds<4>(bs, to->s + wave * 256, rs * 2 + t % 2 * 4 < nb ? min(t / 2, cols - 1) * (uint32_t)A.right_spitch + t % 2 * 4 : kNowhere);
+    }
+
+    // The first group, and in step s (of a pair its second: SECOND) a share of the group after the one that s belongs to.
+    __device__ __forceinline__ void fetch_first(Group* __restrict to) {
+        if constexpr (OP == PRODUCT) { fetch_scales<false>(first, to); fetch_scales<true>(first, to); }
+        if constexpr (OP == LINEAR)
+            for (uint32_t q = 0; q < 4; q++) fetch_quarter(right0, q, to);
+    }
+    template <bool SECOND> __device__ __forceinline__ void fetch_share(uint32_t s, Group* __restrict to) {
+        if constexpr (OP == PRODUCT) fetch_scales<SECOND>(SECOND ? s + 1 : s + 2, to);
+        if constexpr (OP == LINEAR) {                                  // (the same share again for a float's other terms)
+            const uint32_t r = right_step(s) - right0;
+            fetch_quarter(right0 + (r / 4 + 1) * 4, r % 4, to);
         }
     }
 
@@ -228,21 +245,24 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     struct Side { int sl[TM], sr[TN]; i32x4 w[TN]; };
 
     // SECOND: s is the second step of its pair
-    template <bool SECOND> __device__ __forceinline__ void load_side(uint32_t s, const Half* __restrict h, const Scales* __restrict sc, Side& S) {
+    template <bool SECOND> __device__ __forceinline__ void load_side(uint32_t s, const Group* __restrict from, Side& S) {
         if constexpr (OP == PRODUCT) {
             const uint32_t in = nb - min(s * 8 + g * 4, nb);           // blocks of this lane's four that there are
             const int keep = in >= 4 ? -1 : (1 << 8 * in) - 1;
 #pragma unroll
-            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(sc->l + (wm + a * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
+            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(from->s + (wm + a * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
 #pragma unroll
-            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(sc->r + (wj + b * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
+            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(from->r + (wj + b * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
         }
         if constexpr (OP == LINEAR) {
-            const uint32_t blk = right_step(s) * 2 + g;
+            const uint32_t rs = right_step(s), blk = rs * 2 + g;
+            uint32_t at = (rs - right0) % 4 * 2;
+            asm volatile("" : "+s"(at));                               // (not read before the workgroup has met: the group may just have arrived)
+            at += g;
 #pragma unroll
             for (int b = 0; b < TN; b++) {
-                S.w[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + (g ^ l32 / 8 % 2) * 16);
-                const uint32_t sb = h->sr[(wj + b * 32 + l32) * 4 + blk % 4];
+                S.w[b] = *reinterpret_cast<const i32x4*>(from->r + (wj + b * 32 + l32) * 128 + (at ^ l32 / 2 % 8) * 16);
+                const uint32_t sb = from->s[(wj + b * 32 + l32) * 8 + at];
                 S.sr[b] = blk < nb ? sb : 0;
             }
         }
@@ -254,7 +274,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         for (int a = 0; a < TM; a++) F.x[a] = *reinterpret_cast<const i32x4*>(h->l + (wm + a * 32 + l32) * 128 + c);
         if constexpr (OP != LINEAR)
 #pragma unroll
-            for (int b = 0; b < TN; b++) F.y[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * RB + c);
+            for (int b = 0; b < TN; b++) F.y[b] = *reinterpret_cast<const i32x4*>(h->r + (wj + b * 32 + l32) * 128 + c);
     }
 
     // linear: the right's part of a fragment, from four bits.
@@ -313,15 +333,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 
     // Step s, whose first fragments are in registers already.  The workgroup meets while the last of its four multiplications is still to
     // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.  (grad: P holds step s + 1
-    // of the right, and then gets step s + 3.  product: sc has the scales of this pair of steps, and sn is filled with the next one's, one side in
-    // either step.)
-    template <bool SECOND> __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, Scales* __restrict sc, Scales* __restrict sn, Piece& P,
-                                                                Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
+    // of the right, and then gets step s + 3.  `from` is the group of step s + 1, `to` the one after the group of s: they are the same where s is
+    // its group's last step.)
+    template <bool SECOND> __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, const Group* __restrict from,
+                                                                Group* __restrict to, Piece& P, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
         Frag F1, F2, F3;
         load_frag(1, cur, F1);
         widen<1>(S, F1);
-        fetch_rest(s + 1, next);
-        fetch_scales<SECOND>(SECOND ? s + 1 : s + 2, sn);
+        fetch_right(s + 1, next);
+        fetch_share<SECOND>(s, to);
         multiply<0>(F, S, acc);
         order<kGap, 2>();
         load_frag(2, cur, F2);
@@ -337,7 +357,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         fetch_piece(s + 3, P);
         fetch(s + 2, cur);
         Side S1;
-        load_side<!SECOND>(s + 1, next, SECOND ? sn : sc, S1);
+        load_side<!SECOND>(s + 1, from, S1);
         load_frag(0, next, F);
         widen<0>(S1, F);
         multiply<3>(F3, S, acc);
@@ -402,8 +422,7 @@ template <int OP, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     typedef Tile<OP, BM, BN, WM, WN> Tl;
     __shared__ __attribute__((aligned(16))) typename Tl::Half h0, h1;
-    __shared__ __attribute__((aligned(16))) typename Tl::Scales scales[2];
-    typename Tl::Scales *sc = scales, *sn = scales + 1;
+    __shared__ __attribute__((aligned(16))) typename Tl::Group groups[2];
     Tl T(A);
     f32x16 acc[Tl::TM][Tl::TN];
 #pragma unroll
@@ -415,25 +434,23 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_mx_tile(TileArgs A) {
     T.fetch_piece(s, P0);
     T.fetch_piece(s + 1, P1);
     T.fetch(s, &h0);
-    T.fetch_rest(s, &h0);
-    T.template fetch_scales<false>(s, sc);
-    T.template fetch_scales<true>(s, sc);
+    T.fetch_right(s, &h0);
+    T.fetch_first(groups);
     T.fetch(s + 1, &h1);
     T.turn(P0, &h0);
     T.fetch_piece(s + 2, P0);
     T.meet();
     typename Tl::Frag F;
     typename Tl::Side S;
-    T.template load_side<false>(s, &h0, sc, S);
+    T.template load_side<false>(s, groups, S);
     T.load_frag(0, &h0, F);
     T.template widen<0>(S, F);
+    const auto group = [&](uint32_t number) { return groups + number % 2; };
     for (; s + 1 < T.steps; s += 2) {
-        T.template step<false>(s, &h0, &h1, sc, sn, P1, F, S, acc);
-        T.template step<true>(s + 1, &h1, &h0, sc, sn, P0, F, S, acc);
-        typename Tl::Scales* const was = sc;
-        sc = sn; sn = was;
+        T.template step<false>(s, &h0, &h1, group(T.group_of(s + 1)), group(T.group_of(s) + 1), P1, F, S, acc);
+        T.template step<true>(s + 1, &h1, &h0, group(T.group_of(s + 2)), group(T.group_of(s + 1) + 1), P0, F, S, acc);
     }
-    if (s < T.steps) T.template step<false>(s, &h0, &h1, sc, sn, P1, F, S, acc);
+    if (s < T.steps) T.template step<false>(s, &h0, &h1, group(T.group_of(s + 1)), group(T.group_of(s) + 1), P1, F, S, acc);
     Tl::meet();                                                        // (nor may a load reach shared memory after the workgroup's end)
     uint8_t* const scratch = reinterpret_cast<uint8_t*>(&h0);
     if (A.parts > 1) T.template store<float>(A.sums + T.part * A.M * A.sum_pitch, A.sum_pitch, scratch, acc);
