@@ -894,9 +894,10 @@ __global__ __launch_bounds__(64) void k_mx_join(const float* sums, uint32_t part
 // How a product is laid over the chip: tiles of 256 x 256, one workgroup to a compute unit, or of 128 x 128, two; and the length in parts,
 // whose sums a second kernel joins, where there are fewer tiles than compute units.  The least of these estimates in microseconds is taken:
 // a step of a tile takes `alone` where few of them run, and `share` more where each compute unit has one (two of 128 x 128: twice
-// that), since all draw on the same caches and the same power.  Against the best of all tiles and parts on 64 shapes (40 to 4096 rows, sides
-// of 1024 to 8192) the choice costs 1.3 % on average and 16 % at most.  For instance bf16 on the left, 256 rows through 4096 x 4096: tiles of
-// 128 34.2 us and in four parts 25.6, tiles of 256 70.5; 2048 rows through 8192 x 8192: 262.4, of 256 198.3.
+// that), since all draw on the same caches and the same power.  Against the best of all tiles and parts on 66 shapes (40 to 4096 rows, sides
+// of 1024 to 8192) the choice costs 1.3 % on average with operands in the caches, and 7 % at most but
+// for few tiles in four bits (512 rows through 1024 x 4096, four parts 14.6 us, one 12.2; from memory 15.5 and 15.8).  For instance bf16 on the left, 256 rows through 4096 x 4096: tiles of
+// 128 37.6 us and in four parts 24.9, tiles of 256 73.9; 2048 rows through 8192 x 8192: 231.0, of 256 194.0.
 struct Plan { uint32_t tile, parts; };
 struct StepCost { float alone128, share128, alone256, share256; };
 constexpr StepCost kStepCost[3] = { { 0.60f, 0.30f, 1.40f, 0.75f }, { 0.42f, 0.30f, 1.15f, 0.45f }, { 0.80f, 0.25f, 1.45f, 0.28f } };
