@@ -868,9 +868,9 @@ __global__ __launch_bounds__(512, 2) void k_mx_grad_rows(RowArgs A, uint32_t par
     }
 }
 
-// Rows up to which k_mx_rows is taken.  Against 4096 x 4096 in four bits and with bf16, in microseconds: 32 rows 8.1 and 11.6, by tiles 13.3
-// and 16.4; 64 rows (with room for them in its registers) 11.8 and 19.1, by tiles 13.2 and 18.7, against 8192 x 8192 24.9 and 39.1, by
-// tiles 20.2 and 33.0.
+// Rows up to which k_mx_rows is taken.  Against 4096 x 4096 in four bits and with bf16, in microseconds: 32 rows 8.0 and 11.7, by tiles 11.5
+// and 14.8; 64 rows (with room for them in its registers) 11.8 and 19.1, by tiles 12.6 and 17.3, against 8192 x 8192 24.9 and 39.1, by
+// tiles 20.0 and 30.0.
 constexpr uint64_t kFewRows = 32;
 constexpr uint64_t kFewGradRows = 16;
 
@@ -895,9 +895,9 @@ __global__ __launch_bounds__(64) void k_mx_join(const float* sums, uint32_t part
 // whose sums a second kernel joins, where there are fewer tiles than compute units.  The least of these estimates in microseconds is taken:
 // a step of a tile takes `alone` where few of them run, and `share` more where each compute unit has one (two of 128 x 128: twice
 // that), since all draw on the same caches and the same power.  Against the best of all tiles and parts on 66 shapes (40 to 4096 rows, sides
-// of 1024 to 8192) the choice costs 1.3 % on average with operands in the caches, and 7 % at most but
-// for few tiles in four bits (512 rows through 1024 x 4096, four parts 14.6 us, one 12.2; from memory 15.5 and 15.8).  For instance bf16 on the left, 256 rows through 4096 x 4096: tiles of
-// 128 37.6 us and in four parts 24.9, tiles of 256 73.9; 2048 rows through 8192 x 8192: 231.0, of 256 194.0.
+// of 1024 to 8192, operands in the caches) the choice costs 1.3 % on average, and 8 % at most but for few tiles in four bits (512 rows through
+// 1024 x 4096: in four parts 14.6 us, in one 12.2; with operands from memory 15.5 and 15.8).  For instance bf16 on the left, 256 rows through
+// 4096 x 4096: tiles of 128 37.6 us and in four parts 24.9, tiles of 256 73.9; 2048 rows through 8192 x 8192: 231.0, of 256 194.0.
 struct Plan { uint32_t tile, parts; };
 struct StepCost { float alone128, share128, alone256, share256; };
 constexpr StepCost kStepCost[3] = { { 0.60f, 0.30f, 1.40f, 0.75f }, { 0.42f, 0.30f, 1.15f, 0.45f }, { 0.80f, 0.25f, 1.45f, 0.28f } };
