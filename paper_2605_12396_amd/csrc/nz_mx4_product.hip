@@ -103,7 +103,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     uint32_t part, first, steps;                                       // this workgroup's steps: from `first` to below `steps`
     uint32_t right0;                                                   // linear: the right's first step, an even number
     uint32_t lo[LL], ro[RL ? RL : 1], slo[SL ? SL : 1], sro[SR ? SR : 1];
-    uint32_t lchunk;
+    uint32_t lchunk, sword;                                            // the chunk, and the word of a pair's scales, that this thread's loads take
     uint32_t gd, gq;                                                   // grad: rows 2 gd, 2 gd + 1 and columns PW gq .. of a piece
 
     __device__ __forceinline__ explicit Tile(const TileArgs& args) : A(args) {
@@ -127,14 +127,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         left_s = A.left_scales + m0 * A.left_spitch;
         right_s = OP == GRAD ? A.right_scales + j0 / 32 : A.right_scales + j0 * A.right_spitch;
         lchunk = t % 8 ^ t / 16 % 8;
+        sword = t % 4 ^ wave % 2 * 2;
 #pragma unroll
         for (int i = 0; i < LL; i++) lo[i] = min(t / 8 + NT / 8 * i, rows - 1) * (uint32_t)A.left_pitch + lchunk * 16;
 #pragma unroll
         for (int i = 0; i < RL; i++) ro[i] = min(t / 8 + NT / 8 * i, cols - 1) * (uint32_t)A.right_pitch + lchunk * 16;
 #pragma unroll
-        for (int i = 0; i < SL; i++) slo[i] = min(t / 4 + NT / 4 * i, rows - 1) * (uint32_t)A.left_spitch + t % 4 * 4;
+        for (int i = 0; i < SL; i++) slo[i] = min(t / 4 + NT / 4 * i, rows - 1) * (uint32_t)A.left_spitch + sword * 4;
 #pragma unroll
-        for (int i = 0; i < SR; i++) sro[i] = min(t / 4 + NT / 4 * i, cols - 1) * (uint32_t)A.right_spitch + t % 4 * 4;
+        for (int i = 0; i < SR; i++) sro[i] = min(t / 4 + NT / 4 * i, cols - 1) * (uint32_t)A.right_spitch + sword * 4;
         gd = t % 32; gq = t / 32;
     }
 
@@ -196,7 +197,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     // A share of a group.  product: the scales of one side for steps s and s + 1.  linear: quarter q of the rows, from step rs of the right on.
     template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Group* __restrict to) {
         const rsrc_t b = buffer_at((RIGHT ? right_s : left_s) + (uint64_t)s * 8);
-        const bool in = (s < steps) & (s * 8 + t % 4 * 4 < nb);
+        const bool in = (s < steps) & (s * 8 + sword * 4 < nb);
 #pragma unroll
         for (int i = 0; i < (RIGHT ? SR : SL); i++)
             load_lds<4>(b, (RIGHT ? to->r : to->s) + (i * NT + wave * 64) * 4, in ? (RIGHT ? sro : slo)[i] : kNowhere);
@@ -249,10 +250,11 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         if constexpr (OP == PRODUCT) {
             const uint32_t in = nb - min(s * 8 + g * 4, nb);           // blocks of this lane's four that there are
             const int keep = in >= 4 ? -1 : (1 << 8 * in) - 1;
+            const uint32_t at = (SECOND ^ l32 / 16) * 8 + g * 4;       // (the pair's two steps change places every 16 rows, so that all banks are used)
 #pragma unroll
-            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(from->s + (wm + a * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
+            for (int a = 0; a < TM; a++) S.sl[a] = *reinterpret_cast<const int*>(from->s + (wm + a * 32 + l32) * 16 + at) & keep;
 #pragma unroll
-            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(from->r + (wj + b * 32 + l32) * 16 + SECOND * 8 + g * 4) & keep;
+            for (int b = 0; b < TN; b++) S.sr[b] = *reinterpret_cast<const int*>(from->r + (wj + b * 32 + l32) * 16 + at) & keep;
         }
         if constexpr (OP == LINEAR) {
             const uint32_t rs = right_step(s), blk = rs * 2 + g;
