@@ -145,7 +145,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // Sends for step s: the left (grad: all), and the rest.  What lies past the end of a row comes as zeros, and all of a step past the last.
-    __device__ __forceinline__ void fetch(uint32_t s, Half* __restrict h) {
+    __device__ __forceinline__ void fetch(uint32_t s, Half* h) {
         const uint32_t rs = right_step(s);
         const rsrc_t bl = buffer_at(left + (uint64_t)s * 128);
         const bool on = s < steps;
@@ -180,7 +180,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // product: the right for step s.
-    __device__ __forceinline__ void fetch_right(uint32_t s, Half* __restrict h) {
+    __device__ __forceinline__ void fetch_right(uint32_t s, Half* h) {
         if constexpr (OP == PRODUCT) {
             const rsrc_t br = buffer_at(right + (uint64_t)s * 128);
             const bool in = (s < steps) & (s * 8 + lchunk < nb);
@@ -195,14 +195,14 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // A share of a group.  product: the scales of one side for steps s and s + 1.  linear: quarter q of the rows, from step rs of the right on.
-    template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Group* __restrict to) {
+    template <bool RIGHT> __device__ __forceinline__ void fetch_scales(uint32_t s, Group* to) {
         const rsrc_t b = buffer_at((RIGHT ? right_s : left_s) + (uint64_t)s * 8);
         const bool in = (s < steps) & (s * 8 + sword * 4 < nb);
 #pragma unroll
         for (int i = 0; i < (RIGHT ? SR : SL); i++)
             load_lds<4>(b, (RIGHT ? to->r : to->s) + (i * NT + wave * 64) * 4, in ? (RIGHT ? sro : slo)[i] : kNowhere);
     }
-    __device__ __forceinline__ void fetch_quarter(uint32_t rs, uint32_t q, Group* __restrict to) {
+    __device__ __forceinline__ void fetch_quarter(uint32_t rs, uint32_t q, Group* to) {
         const rsrc_t br = buffer_at(right + (uint64_t)rs * 32), bs = buffer_at(right_s + (uint64_t)rs * 2);
         const uint32_t row = min(t / 8 + NT / 8 * q, cols - 1);
         load_lds<16>(br, to->r + (q * NT + wave * 64) * 16, rs * 2 + lchunk < nb ? row * (uint32_t)A.right_pitch + lchunk * 16 : kNowhere);
@@ -211,12 +211,12 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // The first group, and in step s (of a pair its second: SECOND) a share of the group after the one that s belongs to.
-    __device__ __forceinline__ void fetch_first(Group* __restrict to) {
+    __device__ __forceinline__ void fetch_first(Group* to) {
         if constexpr (OP == PRODUCT) { fetch_scales<false>(first, to); fetch_scales<true>(first, to); }
         if constexpr (OP == LINEAR)
             for (uint32_t q = 0; q < 4; q++) fetch_quarter(right0, q, to);
     }
-    template <bool SECOND> __device__ __forceinline__ void fetch_share(uint32_t s, Group* __restrict to) {
+    template <bool SECOND> __device__ __forceinline__ void fetch_share(uint32_t s, Group* to) {
         if constexpr (OP == PRODUCT) fetch_scales<SECOND>(SECOND ? s + 1 : s + 2, to);
         if constexpr (OP == LINEAR) {                                  // (the same share again for a float's other terms)
             const uint32_t r = right_step(s) - right0;
@@ -225,7 +225,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     }
 
     // grad: two rows of codes become columns of bf16, two rows to a word.
-    __device__ __forceinline__ void turn(const Piece& P, Half* __restrict h) {
+    __device__ __forceinline__ void turn(const Piece& P, Half* h) {
         if constexpr (OP == GRAD) {
             const float s0 = mx_scale(P.s[0]), s1 = mx_scale(P.s[1]);
 #pragma unroll
@@ -246,7 +246,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     struct Side { int sl[TM], sr[TN]; i32x4 w[TN]; };
 
     // SECOND: s is the second step of its pair
-    template <bool SECOND> __device__ __forceinline__ void load_side(uint32_t s, const Group* __restrict from, Side& S) {
+    template <bool SECOND> __device__ __forceinline__ void load_side(uint32_t s, const Group* from, Side& S) {
         if constexpr (OP == PRODUCT) {
             const uint32_t in = nb - min(s * 8 + g * 4, nb);           // blocks of this lane's four that there are
             const int keep = in >= 4 ? -1 : (1 << 8 * in) - 1;
@@ -258,9 +258,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         }
         if constexpr (OP == LINEAR) {
             const uint32_t rs = right_step(s), blk = rs * 2 + g;
-            uint32_t at = (rs - right0) % 4 * 2;
-            asm volatile("" : "+s"(at));                               // (not read before the workgroup has met: the group may just have arrived)
-            at += g;
+            const uint32_t at = (rs - right0) % 4 * 2 + g;
 #pragma unroll
             for (int b = 0; b < TN; b++) {
                 S.w[b] = *reinterpret_cast<const i32x4*>(from->r + (wj + b * 32 + l32) * 128 + (at ^ l32 / 2 % 8) * 16);
@@ -270,7 +268,7 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
         }
     }
 
-    __device__ __forceinline__ void load_frag(int j, const Half* __restrict h, Frag& F) {
+    __device__ __forceinline__ void load_frag(int j, const Half* h, Frag& F) {
         const uint32_t c = ((g * 4 + j) ^ l32 / 2 % 8) * 16;
 #pragma unroll
         for (int a = 0; a < TM; a++) F.x[a] = *reinterpret_cast<const i32x4*>(h->l + (wm + a * 32 + l32) * 128 + c);
@@ -304,13 +302,15 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
 
     static __device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
-    // This wave's loads have arrived, its reads and writes of shared memory are done, and so are everyone's.
+    // This wave's loads have arrived, its reads and writes of shared memory are done, and so are everyone's.  The fences keep the compiler from
+    // moving reads and writes across; they reach shared memory through any pointer, since none here is declared to be the only one to its memory
+    // (what a direct load brings is read through another, and `from` and `to` of a step may be one).
     static __device__ __forceinline__ void meet() {
         pin();
-        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0070);                            // vmcnt(0), lgkmcnt(0)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         pin();
     }
 
@@ -337,8 +337,8 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     // come: from then on `cur` is free for step s + 2, and the first fragments of step s + 1 can be read from `next`.  (grad: P holds step s + 1
     // of the right, and then gets step s + 3.  `from` is the group of step s + 1, `to` the one after the group of s: they are the same where s is
     // its group's last step.)
-    template <bool SECOND> __device__ __forceinline__ void step(uint32_t s, Half* __restrict cur, Half* __restrict next, const Group* __restrict from,
-                                                                Group* __restrict to, Piece& P, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
+    template <bool SECOND> __device__ __forceinline__ void step(uint32_t s, Half* cur, Half* next, const Group* from,
+                                                                Group* to, Piece& P, Frag& F, Side& S, f32x16 (&acc)[TM][TN]) {
         Frag F1, F2, F3;
         load_frag(1, cur, F1);
         widen<1>(S, F1);
