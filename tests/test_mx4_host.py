@@ -182,3 +182,16 @@ def test_binding_refuses_host_tensors(nz):
                           (torch.zeros(64, 4, dtype=torch.uint8).t(), torch.zeros(4, 4, dtype=torch.uint8))):
         with pytest.raises(ValueError):
             nz.Mx4(codes, scales)
+
+
+def test_a_length_is_not_parted_more_than_it_can_be(nz):
+    """Floats on the left: their terms of bfloat16, in rows of whole steps of 64 elements, and float32 sums for every part of the length.  A part
+    is made of pairs of such steps, so that there are no more sums than pairs (a workgroup without steps would write sums of zeros)."""
+    import torch
+    rng = np.random.default_rng(0)
+    for left, terms in ((torch.bfloat16, 1), (torch.float16, 2), (torch.float32, 3)):
+        for m, n, k in [(58, 1674, 226), (40, 128, 65), (33, 64, 64)] + [tuple(int(v) for v in np.exp(rng.uniform(np.log(33), np.log(4096), 3))) for _ in range(500)]:
+            chunks = -(-k // 64)
+            pairs = -(-chunks // 2)
+            most = chunks * 128 * terms * m + (pairs * m * -(-n // 4) * 4 * 4 if pairs > 1 else 0)
+            assert nz.nz_mx4_workspace_bytes(nz.MX4_LINEAR, left, m, n, k) <= most, (left, m, n, k)
