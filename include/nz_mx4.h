@@ -62,7 +62,8 @@ size_t nz_mx4_pitch(size_t cols);
 nz_status nz_mx4_quantize(const void* d_in, nz_float_type type, size_t rows, size_t cols, size_t ld, nz_mx4_rounding rounding,
                           uint32_t seed, const nz_mx4_matrix* out, void* stream);
 
-/* The floats that a matrix stands for: exact in NZ_F32 and NZ_BF16, rounded once (to nearest even) in NZ_F16. */
+/* The floats that a matrix stands for: exact in NZ_F32 and NZ_BF16, rounded once (to nearest even) in NZ_F16.  Magnitudes of 2^128 and more (4 and
+ * 6 under s = 253; 2, 3, 4 and 6 under s = 254; no call here writes such a scale) are infinite in all three, and so they are in the sums below. */
 nz_status nz_mx4_dequantize(const nz_mx4_matrix* in, size_t rows, size_t cols, void* d_out, nz_float_type type, size_t ld,
                             void* stream);
 
@@ -90,9 +91,9 @@ nz_status nz_mx4_product(const nz_mx4_matrix* a, const nz_mx4_matrix* b, size_t 
                          nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream);
 
 /* The same with floats on the left: C = X B^T, X[m][k] = d_x[m * ldx + k] of type x_type.  X is not rounded,
- * but bits of a float32 below 2^-133 are cut off (it is multiplied in terms of bfloat16).  Elements of B past the range of float32, 4 and 6
- * times 2^127, are infinite in nz_mx4_dequantize; here and in nz_mx4_grad their products are not finite (infinite, or NaN as those of an
- * infinity and 0). */
+ * but bits of a float32 below 2^-133 are cut off (it is multiplied in terms of bfloat16).  Elements of B of 2^128 and more, which are infinite in
+ * nz_mx4_dequantize, have no finite products here and in nz_mx4_grad (infinite, or NaN as those of an infinity and 0); nz_mx4_product
+ * multiplies them as they are. */
 nz_status nz_mx4_linear(const void* d_x, nz_float_type x_type, size_t ldx, const nz_mx4_matrix* b, size_t M, size_t N, size_t K,
                         void* d_c, nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream);
 

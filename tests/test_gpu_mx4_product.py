@@ -415,3 +415,35 @@ def test_products_in_a_graph(nz):
             step(ew, ey)
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) and p.abs().sum() > 0 for p, q in zip(got, ey))
+
+
+@pytest.mark.parametrize("m", [1, 20, 40])
+@pytest.mark.parametrize("s,code,value", [(253, 5, 3.0), (253, 6, 4.0), (253, 7, 6.0), (254, 3, 1.5), (254, 4, 2.0), (254, 5, 3.0), (254, 7, 6.0)])
+def test_the_border_of_float32s_range(nz, s, code, value, m):
+    """The last weights that float32 holds and the first that it does not: 2^128 is the border.  One element of each row of the left is
+    2^-20, the rest 0, so that what is finite is exact."""
+    import torch
+    n, k = 48, 96
+    codes, scales = np.full((n, k // 2), code * 17, np.uint8), np.full((n, k // 32), s, np.uint8)
+    weight = value * 2.0 ** (s - 127)
+    finite = weight < 2.0 ** 128
+    bm = mat(nz, *R.place(codes, scales, k))
+    y = torch.zeros(n, k, device="cuda:0")
+    assert nz.nz_mx4_dequantize(bm, n, k, y, k) == 0
+    assert (y == (weight if finite else float("inf"))).all()
+    a = np.zeros((m, k // 2), np.uint8), np.full((m, k // 32), 107, np.uint8)        # 2^-20
+    a[0][:, 3] = 2
+    check(nz, nz.MX4_PRODUCT, mat(nz, *R.place(*a, k)), bm, m, n, k, "f32", np.full((m, n), weight * 2.0 ** -20))
+    for left in ("bf16", "f16", "f32"):
+        for kind, call, inner, outer in ((nz.MX4_LINEAR, nz.nz_mx4_linear, k, n), (nz.MX4_GRAD, nz.nz_mx4_grad, n, k)):
+            x = np.zeros((m, inner))
+            x[:, 5] = 2.0 ** -20
+            t = floats(nz, x, left)[0]
+            if finite:
+                check(nz, kind, t, bm, m, n, k, "f32", np.full((m, outer), weight * 2.0 ** -20))
+            else:
+                c = torch.zeros(m, outer, device="cuda:0")
+                wsb = nz.nz_mx4_workspace_bytes(kind, t.dtype, m, n, k)
+                ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device="cuda:0")
+                assert call(t, inner, bm, m, n, k, c, outer, ws, wsb) == 0
+                assert not c.isfinite().any()
