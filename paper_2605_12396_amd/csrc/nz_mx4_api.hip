@@ -89,7 +89,7 @@ bool product_shape_ok(uint64_t M, uint64_t N, uint64_t K) {
 }
 
 bool product_matrix_ok(const nz_mx4_matrix* m, uint64_t rows, uint64_t cols) {
-    return matrix_ok(m, rows, cols) && m->pitch * 16 <= kMaxRowBytes;
+    return matrix_ok(m, rows, cols) && m->pitch <= kMaxRowBytes / 16;          // (of one row, too)
 }
 
 bool product_floats_ok(const void* p, int type, uint64_t cols, uint64_t ld) {

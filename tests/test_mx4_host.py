@@ -195,3 +195,14 @@ def test_a_length_is_not_parted_more_than_it_can_be(nz):
             pairs = -(-chunks // 2)
             most = chunks * 128 * terms * m + (pairs * m * -(-n // 4) * 4 * 4 if pairs > 1 else 0)
             assert nz.nz_mx4_workspace_bytes(nz.MX4_LINEAR, left, m, n, k) <= most, (left, m, n, k)
+
+
+def test_products_refuse_a_single_row_that_is_too_long(nz):
+    """The row length of a matrix of one row is held to the same limit, and its bytes do not pass 64 bits unseen."""
+    L, W = nz.lib(), 1 << 23
+    for pitch in ((1 << 18) + 4, 1 << 60, (1 << 60) + 8, (1 << 64) - 4):
+        long_, short = _mat(nz, pitch=pitch), _mat(nz, pitch=8)
+        assert L.nz_mx4_product(long_, short, 1, 40, 200, P, 0, 40, W, 1 << 40, None) == nz.ERR_INVALID, pitch
+        assert L.nz_mx4_product(short, long_, 5, 1, 200, P, 0, 1, W, 1 << 40, None) == nz.ERR_INVALID, pitch
+        assert L.nz_mx4_linear(P, 1, 200, long_, 5, 1, 200, P, 0, 1, W, 1 << 40, None) == nz.ERR_INVALID, pitch
+        assert L.nz_mx4_grad(P, 1, 1, long_, 5, 1, 200, P, 0, 200, W, 1 << 40, None) == nz.ERR_INVALID, pitch
