@@ -83,9 +83,9 @@ nz_status sum_to(const nz_mx4_matrix* in, uint32_t k, const float* d_local, uint
     return sum_to<kMxMaxOperands>(in, k, d_local, ld_local, rows, cols, O, stream);
 }
 
-bool product_shape_ok(uint64_t M, uint64_t N, uint64_t K) {
+bool product_shape_ok(int kind, uint64_t M, uint64_t N, uint64_t K) {
     return M > 0 && N > 0 && K > 0 && M < kMaxProductSide && N < kMaxProductSide && K < kMaxProductSide && M * N < kMaxOutput &&
-           M * K < kMaxOutput;
+           M * K < (kind == NZ_MX4_PRODUCT ? kMaxElements : kMaxOutput) && N * K < kMaxElements;
 }
 
 bool product_matrix_ok(const nz_mx4_matrix* m, uint64_t rows, uint64_t cols) {
@@ -149,13 +149,13 @@ nz_status nz_mx4_reduce_k(const nz_mx4_matrix* in, uint32_t k, const float* d_lo
 
 size_t nz_mx4_workspace_bytes(nz_mx4_kind kind, nz_float_type left, size_t M, size_t N, size_t K) {
     const bool kind_ok = kind == NZ_MX4_PRODUCT || kind == NZ_MX4_LINEAR || kind == NZ_MX4_GRAD;
-    if (!kind_ok || (kind != NZ_MX4_PRODUCT && !is_float_type(left)) || !product_shape_ok(M, N, K)) return (size_t)-1;
+    if (!kind_ok || (kind != NZ_MX4_PRODUCT && !is_float_type(left)) || !product_shape_ok(kind, M, N, K)) return (size_t)-1;
     return mx_product_workspace(kind, left, M, N, K);
 }
 
 nz_status nz_mx4_product(const nz_mx4_matrix* a, const nz_mx4_matrix* b, size_t M, size_t N, size_t K, void* d_c,
                          nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream) {
-    if (!product_shape_ok(M, N, K) || !product_matrix_ok(a, M, K) || !product_matrix_ok(b, N, K) || !product_floats_ok(d_c, type, N, ldc))
+    if (!product_shape_ok(NZ_MX4_PRODUCT, M, N, K) || !product_matrix_ok(a, M, K) || !product_matrix_ok(b, N, K) || !product_floats_ok(d_c, type, N, ldc))
         return NZ_ERR_INVALID;
     MxProductArgs A = {};
     A.a = { reinterpret_cast<const uint8_t*>(a->codes), reinterpret_cast<const uint8_t*>(a->scales), a->pitch };
@@ -164,7 +164,7 @@ nz_status nz_mx4_product(const nz_mx4_matrix* a, const nz_mx4_matrix* b, size_t 
 
 nz_status nz_mx4_linear(const void* d_x, nz_float_type x_type, size_t ldx, const nz_mx4_matrix* b, size_t M, size_t N, size_t K,
                         void* d_c, nz_float_type type, size_t ldc, void* d_ws, size_t ws_bytes, void* stream) {
-    if (!product_shape_ok(M, N, K) || !product_floats_ok(d_x, x_type, K, ldx) || !product_matrix_ok(b, N, K) ||
+    if (!product_shape_ok(NZ_MX4_LINEAR, M, N, K) || !product_floats_ok(d_x, x_type, K, ldx) || !product_matrix_ok(b, N, K) ||
         !product_floats_ok(d_c, type, N, ldc)) return NZ_ERR_INVALID;
     MxProductArgs A = {};
     A.x = d_x; A.ldx = ldx;
@@ -173,7 +173,7 @@ nz_status nz_mx4_linear(const void* d_x, nz_float_type x_type, size_t ldx, const
 
 nz_status nz_mx4_grad(const void* d_g, nz_float_type g_type, size_t ldg, const nz_mx4_matrix* b, size_t M, size_t N, size_t K,
                       void* d_da, nz_float_type type, size_t ldda, void* d_ws, size_t ws_bytes, void* stream) {
-    if (!product_shape_ok(M, N, K) || !product_floats_ok(d_g, g_type, N, ldg) || !product_matrix_ok(b, N, K) ||
+    if (!product_shape_ok(NZ_MX4_GRAD, M, N, K) || !product_floats_ok(d_g, g_type, N, ldg) || !product_matrix_ok(b, N, K) ||
         !product_floats_ok(d_da, type, K, ldda)) return NZ_ERR_INVALID;
     MxProductArgs A = {};
     A.x = d_g; A.ldx = ldg;

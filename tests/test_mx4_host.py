@@ -206,3 +206,22 @@ def test_products_refuse_a_single_row_that_is_too_long(nz):
         assert L.nz_mx4_product(short, long_, 5, 1, 200, P, 0, 1, W, 1 << 40, None) == nz.ERR_INVALID, pitch
         assert L.nz_mx4_linear(P, 1, 200, long_, 5, 1, 200, P, 0, 1, W, 1 << 40, None) == nz.ERR_INVALID, pitch
         assert L.nz_mx4_grad(P, 1, 1, long_, 5, 1, 200, P, 0, 200, W, 1 << 40, None) == nz.ERR_INVALID, pitch
+
+
+def test_products_refuse_matrices_of_2_to_the_38_elements(nz):
+    """The limit of a matrix holds for those of the products as well (sides and rows within theirs)."""
+    import torch
+    L, W = nz.lib(), 1 << 23
+    n, k = 1 << 18, 1 << 20                                # rows of 512 KB of codes
+    wide = _mat(nz, pitch=k // 32)
+    assert L.nz_mx4_product(wide, wide, 5, n, k, P, 0, n, W, 1 << 50, None) == nz.ERR_INVALID
+    assert L.nz_mx4_product(wide, wide, n, 5, k, P, 0, 5, W, 1 << 50, None) == nz.ERR_INVALID
+    assert L.nz_mx4_linear(P, 1, k, wide, 5, n, k, P, 0, n, W, 1 << 50, None) == nz.ERR_INVALID
+    assert L.nz_mx4_grad(P, 1, n, wide, 5, n, k, P, 0, k, W, 1 << 50, None) == nz.ERR_INVALID
+    for kind, left in ((nz.MX4_PRODUCT, None), (nz.MX4_LINEAR, torch.bfloat16), (nz.MX4_GRAD, torch.bfloat16)):
+        with pytest.raises(ValueError):
+            nz.nz_mx4_workspace_bytes(kind, left, 5, n, k)
+        assert nz.nz_mx4_workspace_bytes(kind, left, 5, n - 1, k) >= 0
+    with pytest.raises(ValueError):
+        nz.nz_mx4_workspace_bytes(nz.MX4_PRODUCT, None, n, 5, k)
+    assert nz.nz_mx4_workspace_bytes(nz.MX4_LINEAR, torch.bfloat16, n, 5, k) >= 0        # (floats: below 2^40)
