@@ -283,3 +283,37 @@ def test_offsets_past_32_bits(nz):
             want = torch.from_numpy(R.values(codes[i:i + 1], scales[i:i + 1], c)).to(torch.bfloat16)
             assert torch.equal(y[r:r + 1, :c].cpu(), want), (c, r)
         del m, y
+
+
+def test_more_rows_than_one_layer_of_the_grid(nz):
+    """Rows are laid over the grid in groups of fewer than 2^29 blocks; past that a second group starts, whose draws, rows and shorter end are its
+    own.  2^29 + 5 rows of one block: rows on either side of the border, and at both ends."""
+    import torch
+    rows, cols = (1 << 29) + 5, 2
+    base = torch.randn(1 << 20, cols, device="cuda:0").bfloat16()
+    x = base.repeat(-(-rows // base.shape[0]), 1)[:rows]
+    m = nz.Mx4(torch.empty(rows, 64, dtype=torch.uint8, device="cuda:0"), torch.empty(rows, 4, dtype=torch.uint8, device="cuda:0"))
+    y = torch.full((rows + 3, cols), 9.0, dtype=torch.bfloat16, device="cuda:0")
+    border = (1 << 29) - 1                                               # rows of the first group
+    parts = [(0, 3), (border - 3, border), (border, border + 3), (rows - 3, rows)]
+    for stochastic in (0, 1):
+        m.codes.fill_(0xA5)
+        m.scales.fill_(0xA5)
+        assert nz.nz_mx4_quantize(x, rows, cols, cols, stochastic, 23, m) == 0
+        assert nz.nz_mx4_dequantize(m, rows, cols, y, cols) == 0
+        for a, b in parts:
+            rc, rs = R.quantize(x[a:b].double().cpu().numpy(), bool(stochastic), 23, first=a * 32)
+            want_c, want_s = R.place(rc, rs, cols, 0, 0xA5)
+            assert (m.codes[a:b].cpu().numpy() == want_c).all() and (m.scales[a:b].cpu().numpy() == want_s).all(), (a, stochastic)
+            assert torch.equal(y[a:b].cpu(), torch.from_numpy(R.values(rc, rs, cols)).bfloat16()), (a, stochastic)
+        assert (y[rows:] == 9).all()
+    # four bits into four bits, with float32 data of its own
+    local = torch.ones(rows, cols, device="cuda:0")
+    out = nz.Mx4(torch.empty_like(m.codes), torch.empty_like(m.scales))
+    assert nz.nz_mx4_reduce_k([m], local, cols, rows, cols, 1, 29, out) == 0
+    for a, b in parts:
+        want = sum64([R.values(m.codes[a:b].cpu().numpy(), m.scales[a:b].cpu().numpy(), cols)], np.ones((b - a, cols)))
+        rc, rs = R.quantize(want, True, 29, first=a * 32)
+        assert (out.codes[a:b, :16].cpu().numpy() == rc).all() and (out.scales[a:b, :1].cpu().numpy() == rs).all(), a
+    del x, m, y, local, out
+    torch.cuda.empty_cache()
