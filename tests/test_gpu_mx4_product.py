@@ -447,3 +447,26 @@ def test_the_border_of_float32s_range(nz, s, code, value, m):
                 ws = torch.empty(max(wsb, 16), dtype=torch.uint8, device="cuda:0")
                 assert call(t, inner, bm, m, n, k, c, outer, ws, wsb) == 0
                 assert not c.isfinite().any()
+
+
+def test_the_sum_that_a_rank_hands_on(nz):
+    """The last hop of the sharded step: three peers' gradients, rounded without bias, and the rank's own float32 sum, last, go on in four bits."""
+    import torch
+    rng = np.random.default_rng(14)
+    n = 256 * 320
+    sent, values = [], []
+    for r in range(3):
+        g = floats(nz, rng.standard_normal((1, n)) * 0.01, "f32")[0]
+        msg = nz.Mx4.empty(1, n)
+        assert nz.nz_mx4_quantize(g, 1, n, n, nz.MX4_STOCHASTIC, 100 + r, msg) == 0
+        sent.append(msg)
+        values.append(R.values(msg.codes.cpu().numpy(), msg.scales.cpu().numpy(), n).astype(np.float32))
+    mine, mine64 = floats(nz, rng.standard_normal((1, n)) * 0.02, "f32")
+    total = values[0]
+    for v in values[1:] + [mine64.astype(np.float32)]:
+        total = total + v
+    for rounding in (nz.MX4_NEAREST, nz.MX4_STOCHASTIC):
+        out = nz.Mx4(torch.full_like(sent[0].codes, 0xA5), torch.full_like(sent[0].scales, 0xA5))
+        assert nz.nz_mx4_reduce_k(sent, mine, n, 1, n, rounding, 9, out) == 0
+        rc, rs = R.quantize(total.astype(np.float64), bool(rounding), 9)
+        assert (out.codes.cpu().numpy() == rc).all() and (out.scales.cpu().numpy() == rs).all()
