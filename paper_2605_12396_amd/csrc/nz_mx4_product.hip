@@ -580,7 +580,10 @@ __device__ __forceinline__ void store_one(void* c, int type, uint64_t at, float 
 // for four bits (one instruction, group g taking block g).
 // The matrix instructions take 16 rows whether there are as many or not.  FEW: as many rows as few_rows says, which also come through shared
 // memory, each byte loaded and cut into terms once; else every lane loads the fragments that it multiplies, and the next units' codes are on
-// their way meanwhile (FEW has two workgroups on a compute unit instead).
+// their way meanwhile (FEW has room for two workgroups on a compute unit instead, where there are more than 256).  FEW saves the cutting: one
+// row against 8192 x 8192, codes from memory, float32 14.8 us instead of 21.4, fp16 14.5 / 18.8; against 4096 x 4096 7.8 / 10.1 and 7.5 / 9.1.
+// What is not cut gains less or loses: four bits 11.9 / 11.6, four rows 11.9 / 12.5 (codes in the caches 7.6 / 7.8 and 7.7 / 8.8), bf16 14.2 / 13.0
+// (9.6 / 9.4, four rows 10.1 / 10.7); against 4096 x 4096 5.4 / 4.8 and 6.4 / 5.4.
 __host__ __device__ constexpr uint32_t few_rows(int left) { return left < 0 ? 4 : left == F32 ? 1 : left == F16 ? 2 : 4; }
 
 template <int LEFT, int MF, int NJ, bool FEW>
@@ -765,6 +768,10 @@ __global__ __launch_bounds__(512, FEW ? 4 : 2) void k_mx_rows(RowArgs A) {
     }
 }
 
+// Two tiles of 16 columns a workgroup from 512 tiles on, so that half as many workgroups read the left: 16 rows of bf16 through 8192 x 4096
+// 9.8 us, by one tile each 13.9, through 16384 x 4096 18.6 and 26.2, one row there 14.5 and 14.7.  Fewer tiles keep a workgroup each, which fills
+// the chip: 4096 columns 8.0 us, by two 9.1.  Not best for every count of rows near the border: one row of bf16 through 8192 x 4096 takes 9.1, by
+// one tile each 8.2, and 16 rows through 6144 x 4096 13.2, by two 9.4.
 template <int LEFT, int MF, bool FEW> void launch_rows(const RowArgs& R, hipStream_t st) {
     const uint64_t tiles = (R.outer + 15) / 16;
     if (tiles >= 512) hipLaunchKernelGGL((k_mx_rows<LEFT, MF, 2, FEW>), dim3((uint32_t)((tiles + 1) / 2)), dim3(512), 0, st, R);
@@ -877,6 +884,8 @@ __global__ __launch_bounds__(512, 2) void k_mx_grad_rows(RowArgs A, uint32_t par
 // and 14.8; 64 rows (with room for them in its registers) 11.8 and 19.1, by tiles 12.6 and 17.3, against 8192 x 8192 24.9 and 39.1, by
 // tiles 20.0 and 30.0.
 constexpr uint64_t kFewRows = 32;
+// And k_mx_grad_rows, which has registers for no more.  bf16, 16 rows through 4096 x 4096 12.0 us, by tiles 17.5; through 8192 x 8192 20.2 and 33.4;
+// one row 9.2 and 16.3, 16.5 and 32.7.
 constexpr uint64_t kFewGradRows = 16;
 
 // Sums of the parts of a length, in their order, into C: a thread makes four neighbouring columns.
@@ -968,7 +977,8 @@ template <int T> void launch_terms(const MxProductArgs& A, uint64_t inner, uint3
 size_t laid_bytes(int left, uint64_t M, uint64_t inner) { return (M * ((inner + 7) / 8 * 8) * float_bytes(left) + 255) / 256 * 256; }
 
 // Parts of the rows of B in k_mx_grad_rows: a workgroup for every compute unit, 32 rows at least for every wave; not more than one kernel
-// joins quickly.
+// joins quickly: one row through 16384 x 512 10.6 us, in up to 16 parts 11.1, in up to 64 12.3; through 65536 x 1024 19.3, 25.2 and 18.5; through
+// 8192 x 1024 9.8, 9.2 and 9.8.
 uint32_t grad_parts(uint64_t outer, uint64_t inner) {
     const uint64_t strips = (outer + 255) / 256, most = (inner + 255) / 256;
     const uint64_t parts = strips >= 256 ? 1 : 256 / strips;
