@@ -80,7 +80,9 @@ nz_status nz_mx4_sum_k(const nz_mx4_matrix* in, uint32_t k, const float* d_local
                        void* d_out, nz_float_type type, size_t ld, void* stream);
 
 /* Host, pure.  Workspace bytes of the products below (may be 0: then d_ws may be NULL); `left` is the type of the float
- * operand, not used by NZ_MX4_PRODUCT.  (size_t)-1 for sizes that the products refuse. */
+ * operand, not used by NZ_MX4_PRODUCT.  (size_t)-1 for sizes that the products refuse.  Enough for any row length and address: floats of more than
+ * 32 rows (NZ_MX4_GRAD: 16) are laid out in it as terms of bfloat16, and bfloat16 counts too, though rows at multiples of 16 bytes whose length
+ * is a multiple of 8 elements are read where they lie. */
 size_t nz_mx4_workspace_bytes(nz_mx4_kind kind, nz_float_type left, size_t M, size_t N, size_t K);
 
 /*
