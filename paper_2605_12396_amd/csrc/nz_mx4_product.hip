@@ -310,8 +310,8 @@ template <int OP, int BM, int BN, int WM, int WN> struct Tile {
     // (what a direct load brings is read through another, and `from` and `to` of a step may be one).
     static __device__ __forceinline__ void meet() {
         pin();
-        __builtin_amdgcn_s_waitcnt(0x0070);                            // vmcnt(0), lgkmcnt(0)
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");          // (before the wait, so that no load can be sent behind it)
+        __builtin_amdgcn_s_waitcnt(0x0070);                            // vmcnt(0), lgkmcnt(0): direct loads too
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         pin();
